@@ -76,6 +76,8 @@ extern "C" {
 #define SDLLM_OP_COMPACT_KV 1
 #define SDLLM_OP_SPARSE_ATTN 2
 #define SDLLM_OP_BLOCK_STEP 3
+#define SDLLM_OP_SPARSE_ATTN_PACKED 4
+#define SDLLM_OP_BLOCK_STEP_PACKED 5
 
 typedef struct sdllm_shape {
   int32_t batch;       /* B >= 1 */
@@ -127,7 +129,7 @@ int32_t sdllm_retained_count(const sdllm_shape_t* shape, int32_t* k_total, int32
  * take less, down to an amount that depends on their sizes only and often is nothing: they then run fewer key splits or another kernel,
  * as small bf16 calls (head_dim 128, block of 32) of sdllm_sparse_attn do with a workspace that is not aligned to 16 bytes, and
  * the results differ by rounding.  sdllm_sparse_attn and state 2 of sdllm_block_step give the same bits for the same tensors if each
- * is given its full size.
+ * is given its full size.  The operations on a packed cache need all of theirs.
  */
 int32_t sdllm_workspace_bytes(const sdllm_shape_t* shape, int32_t op, int32_t n_cached, size_t* bytes);
 
@@ -221,6 +223,101 @@ int32_t sdllm_block_step(const sdllm_shape_t* shape, int32_t step_in_block, int3
 int32_t sdllm_dense_attn(const sdllm_shape_t* shape, const void* q_full, const int64_t* q_full_stride,
                          const void* k_full, const void* v_full, void* out_full, const int64_t* out_full_stride,
                          void* stream);
+
+/*
+ * ---- A cache of 4 bits a value
+ *
+ * The compacted cache in 4.25 bits a value instead of 16 or 32: written once per block, read at every step that reuses it.  A value is
+ * one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (codes 0 to 7, sign in bit 3) times 2^e.  One e holds for a group of 32 values: 32
+ * neighbouring channels of a key, or one channel of 32 value rows that follow each other in the cache (the last group of a head is filled up
+ * with zeros).  e is the smallest integer in [-125, 125] for which all magnitudes of the group are below 7 2^e; a value becomes the nearest
+ * number, of two equally near ones that with the even code, and the largest number past the end.  A group with an
+ * infinity or a NaN reads as NaN as a whole.  Both types of tensors hold the numbers exactly.
+ *
+ * The cache is one buffer of sdllm_packed_cache_bytes, aligned to 16 bytes, for the rows [0, cache_rows) of every (batch, KV head); the caller
+ * allocates it once for as many rows as it will need.  Per (batch, KV head), densely, ceil(cache_rows / 32) tiles of 34 d bytes:
+ *   32 d/2 bytes  key codes    [d/32 groups g][32 rows][16 bytes]: channels 32 g .. 32 g + 31, the lower four bits first
+ *   32 d/2 bytes  value codes  [d/64: i][2: h][32: m][2: j][8 bytes]: channel (d/32) m + 2 i + j; nibble 4 a + p is row 8 a + 4 h + p
+ *   d bytes       key scales   [32 rows][d/32 groups]: e + 127, or 255 for NaN
+ *   d bytes       value scales [d channels]
+ * Rows past those written of the last tile hold zeros.
+ */
+
+/* Bytes of a packed cache for cache_rows >= 0 rows per (batch, KV head).  Reads batch, n_kv_heads and head_dim of `shape`.  Host call. */
+int32_t sdllm_packed_cache_bytes(const sdllm_shape_t* shape, int32_t cache_rows, size_t* bytes);
+
+/*
+ * sdllm_compact_kv into a packed cache: its rows [0, k_total) become the rows idx[0..k_total) of k_full and v_full ([B,Hkv,L,d],
+ * kv_stride).  cache_rows >= k_total.  idx as for sdllm_compact_kv.
+ */
+int32_t sdllm_compact_kv_packed(const sdllm_shape_t* shape, const void* k_full, const void* v_full, const int32_t* idx, void* cache,
+                                int32_t cache_rows, void* stream);
+
+/* The values of rows [0, n_cached) of a packed cache as rows of k_out and v_out, [B,Hkv,>= n_cached,d] (cache_stride), in the shape's type. */
+int32_t sdllm_unpack_kv(const sdllm_shape_t* shape, const void* cache, int32_t cache_rows, int32_t n_cached, void* k_out, void* v_out,
+                        void* stream);
+
+/*
+ * sdllm_sparse_attn over rows [0, n_cached) of a packed cache and the block's own k_blk/v_blk, which are not packed; n_cached may be 0 (the cache may
+ * be NULL then).  Other arguments as there; ws of sdllm_workspace_bytes(SDLLM_OP_SPARSE_ATTN_PACKED) for the same n_cached, aligned to
+ * 16 bytes.  The cache enters with its exact values; with bf16 tensors the softmax numerators are rounded to bf16 for the product with the values,
+ * with fp32 tensors products and sums are fp32.
+ */
+int32_t sdllm_sparse_attn_packed(const sdllm_shape_t* shape, const void* q_blk, const void* cache, int32_t cache_rows, int32_t n_cached,
+                                 const void* k_blk, const void* v_blk, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * sdllm_block_step with a packed cache: states 0 and 1 are dense attention over k_in/v_in as there, state 1 packs the retained rows
+ * (sdllm_score_select + sdllm_compact_kv_packed), state 2 is sdllm_sparse_attn_packed over k_total rows.  cache_rows >= k_total in states
+ * 1 and 2.  ws of sdllm_workspace_bytes(SDLLM_OP_BLOCK_STEP_PACKED), aligned to 256 bytes.
+ */
+int32_t sdllm_block_step_packed(const sdllm_shape_t* shape, int32_t step_in_block, int32_t delay, const void* q_blk, const void* k_in,
+                                const void* v_in, int32_t* idx, void* cache, int32_t cache_rows, void* out, void* ws, size_t ws_bytes,
+                                void* stream, int32_t* state_out);
+
+/*
+ * ---- Norm of query and key heads and rotation by position
+ *
+ * What a projection goes through on its way to q_blk and k_in.  For each (batch, head, row):
+ *   y = x / sqrt(mean(x^2) + eps) * weight     (SDLLM_NORM_RMS; a null weight is all ones)   or   y = x   (SDLLM_NORM_NONE),
+ * then the pairs (a, b) of its first rot_dim channels are turned by t = position * inv_freq[f], f = 0 .. rot_dim/2 - 1:
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),
+ * pair f being channels (f, f + rot_dim/2) (SDLLM_PAIR_HALVES) or (2 f, 2 f + 1) (SDLLM_PAIR_ADJACENT).  fp32 throughout and one
+ * rounding at the end; t is formed and reduced in 64 bits.
+ */
+#define SDLLM_NORM_NONE 0
+#define SDLLM_NORM_RMS 1
+#define SDLLM_PAIR_HALVES 0
+#define SDLLM_PAIR_ADJACENT 1
+
+typedef struct sdllm_qk_shape {
+  int32_t batch;       /* B >= 1 */
+  int32_t n_q_heads;   /* >= 0 */
+  int32_t n_kv_heads;  /* >= 0, not both 0 */
+  int32_t head_dim;    /* 64 or 128 */
+  int32_t rows;        /* n >= 0 positions */
+  int32_t dtype;       /* SDLLM_BF16 | SDLLM_F32 */
+  int32_t rot_dim;     /* a multiple of 16 in [0, head_dim]; 0: no rotation */
+  int32_t pairing;     /* SDLLM_PAIR_HALVES | SDLLM_PAIR_ADJACENT */
+  int32_t norm;        /* SDLLM_NORM_NONE | SDLLM_NORM_RMS */
+  float eps;           /* >= 0 */
+  int32_t pos_begin;   /* without `positions`: row i is at position pos_begin + i */
+  int32_t reserved;    /* must be 0 */
+  int64_t pos_stride;  /* elements between the batch's rows of `positions`; 0: the same for all */
+  /* element strides {batch, head, row}; the last axis is contiguous */
+  int64_t q_in_stride[3];  /* [B, Hq,  n, d] */
+  int64_t k_in_stride[3];  /* [B, Hkv, n, d] */
+  int64_t q_out_stride[3];
+  int64_t k_out_stride[3];
+} sdllm_qk_shape_t;
+
+/*
+ * q_in/k_in -> q_out/k_out; an output may be its input, with the same strides, and may overlap nothing else.  Tensors of no heads are not read (NULL).
+ * q_weight/k_weight [d] in the tensors' type, 16-byte aligned, or NULL; inv_freq [rot_dim/2] fp32 (NULL if rot_dim is 0);
+ * positions int32 [B, n], n contiguous (pos_stride between batches), of either sign, or NULL.
+ */
+int32_t sdllm_qk_norm_rope(const sdllm_qk_shape_t* shape, const void* q_in, const void* k_in, const void* q_weight, const void* k_weight,
+                           const float* inv_freq, const int32_t* positions, void* q_out, void* k_out, void* stream);
 
 #ifdef __cplusplus
 }

@@ -26,10 +26,15 @@ SDLLM_MAX_POOL, SDLLM_AVG_POOL = 0, 1
 SDLLM_EVICT_BIDIRECTIONAL, SDLLM_EVICT_PREFIX_ONLY = 0, 1
 SDLLM_STATE_FULL, SDLLM_STATE_UPDATE, SDLLM_STATE_REUSE = 0, 1, 2
 SDLLM_OP_SCORE_SELECT, SDLLM_OP_COMPACT_KV, SDLLM_OP_SPARSE_ATTN, SDLLM_OP_BLOCK_STEP = 0, 1, 2, 3
+SDLLM_OP_SPARSE_ATTN_PACKED, SDLLM_OP_BLOCK_STEP_PACKED = 4, 5
+SDLLM_NORM_NONE, SDLLM_NORM_RMS = 0, 1
+SDLLM_PAIR_HALVES, SDLLM_PAIR_ADJACENT = 0, 1
 
 EXPORTED = ("sdllm_error_string", "sdllm_version", "sdllm_retained_count", "sdllm_workspace_bytes",
             "sdllm_cache_state", "sdllm_score_select", "sdllm_compact_kv", "sdllm_sparse_attn",
-            "sdllm_sparse_attn_noalloc", "sdllm_block_step", "sdllm_dense_attn", "sdllm_stream_read_probe",
+            "sdllm_sparse_attn_noalloc", "sdllm_block_step", "sdllm_dense_attn", "sdllm_packed_cache_bytes",
+            "sdllm_compact_kv_packed", "sdllm_unpack_kv", "sdllm_sparse_attn_packed", "sdllm_block_step_packed",
+            "sdllm_qk_norm_rope", "sdllm_stream_read_probe",
             "sdllm_launch_plan", "sdllm_burst_splits", "sdllm_dense_tail_groups",
             "sdllm_column_kernel")
 
@@ -49,6 +54,16 @@ class sdllm_shape_t(ctypes.Structure):
         ("reserved", ctypes.c_int32), ("retention", ctypes.c_double),
         ("q_stride", ctypes.c_int64 * 3), ("kv_stride", ctypes.c_int64 * 3), ("blk_stride", ctypes.c_int64 * 3),
         ("cache_stride", ctypes.c_int64 * 3), ("out_stride", ctypes.c_int64 * 3),
+    ]
+
+
+class sdllm_qk_shape_t(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("rows", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("pairing", ctypes.c_int32),
+        ("norm", ctypes.c_int32), ("eps", ctypes.c_float), ("pos_begin", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("pos_stride", ctypes.c_int64), ("q_in_stride", ctypes.c_int64 * 3), ("k_in_stride", ctypes.c_int64 * 3),
+        ("q_out_stride", ctypes.c_int64 * 3), ("k_out_stride", ctypes.c_int64 * 3),
     ]
 
 
@@ -100,6 +115,18 @@ def load() -> ctypes.CDLL:
     lib.sdllm_block_step.argtypes = [shp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, i32p]
     lib.sdllm_dense_attn.restype = i32
     lib.sdllm_dense_attn.argtypes = [shp, vp, ctypes.POINTER(ctypes.c_int64), vp, vp, vp, ctypes.POINTER(ctypes.c_int64), vp]
+    lib.sdllm_packed_cache_bytes.restype = i32
+    lib.sdllm_packed_cache_bytes.argtypes = [shp, i32, ctypes.POINTER(sz)]
+    lib.sdllm_compact_kv_packed.restype = i32
+    lib.sdllm_compact_kv_packed.argtypes = [shp, vp, vp, vp, vp, i32, vp]
+    lib.sdllm_unpack_kv.restype = i32
+    lib.sdllm_unpack_kv.argtypes = [shp, vp, i32, i32, vp, vp, vp]
+    lib.sdllm_sparse_attn_packed.restype = i32
+    lib.sdllm_sparse_attn_packed.argtypes = [shp, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.sdllm_block_step_packed.restype = i32
+    lib.sdllm_block_step_packed.argtypes = [shp, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, sz, vp, i32p]
+    lib.sdllm_qk_norm_rope.restype = i32
+    lib.sdllm_qk_norm_rope.argtypes = [ctypes.POINTER(sdllm_qk_shape_t), vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.sdllm_stream_read_probe.restype = i32
     lib.sdllm_stream_read_probe.argtypes = [vp, sz, vp, vp]
     lib.sdllm_launch_plan.restype = i32
@@ -206,6 +233,22 @@ def make_shape(*, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, se
     return s
 
 
+def make_qk_shape(*, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, rows: int, dtype: int, rot_dim: Optional[int] = None,
+                  pairing: int = SDLLM_PAIR_HALVES, norm: int = SDLLM_NORM_RMS, eps: float = 1e-6, pos_begin: int = 0,
+                  pos_stride: int = 0, q_in_stride: Optional[Sequence[int]] = None, k_in_stride: Optional[Sequence[int]] = None,
+                  q_out_stride: Optional[Sequence[int]] = None, k_out_stride: Optional[Sequence[int]] = None) -> sdllm_qk_shape_t:
+    """Fill an sdllm_qk_shape_t; strides left out default to dense [B, H, n, d] tensors, rot_dim to the whole head."""
+    s = sdllm_qk_shape_t()
+    s.batch, s.n_q_heads, s.n_kv_heads, s.head_dim, s.rows, s.dtype = batch, n_q_heads, n_kv_heads, head_dim, rows, dtype
+    s.rot_dim, s.pairing, s.norm, s.eps = head_dim if rot_dim is None else rot_dim, pairing, norm, eps
+    s.pos_begin, s.pos_stride, s.reserved = pos_begin, pos_stride, 0
+    for name, val, heads in (("q_in_stride", q_in_stride, n_q_heads), ("k_in_stride", k_in_stride, n_kv_heads),
+                             ("q_out_stride", q_out_stride, n_q_heads), ("k_out_stride", k_out_stride, n_kv_heads)):
+        v = tuple(val) if val is not None else (heads * rows * head_dim, rows * head_dim, head_dim)
+        setattr(s, name, (ctypes.c_int64 * 3)(*v))
+    return s
+
+
 # ------------------------------------------------------------------ the C entry points
 def sdllm_version() -> int:
     return load().sdllm_version()
@@ -283,6 +326,64 @@ def sdllm_dense_attn(shape, q_full, k_full, v_full, out_full, stream=None) -> No
     os_ = (ctypes.c_int64 * 3)(*strides_of(out_full))
     _check(load().sdllm_dense_attn(ctypes.byref(shape), _ptr(q_full), qs, _ptr(k_full), _ptr(v_full), _ptr(out_full), os_,
                                    _stream(stream)), "sdllm_dense_attn")
+
+
+def sdllm_packed_cache_bytes(shape: sdllm_shape_t, cache_rows: int) -> int:
+    out = ctypes.c_size_t()
+    _check(load().sdllm_packed_cache_bytes(ctypes.byref(shape), cache_rows, ctypes.byref(out)), "sdllm_packed_cache_bytes")
+    return out.value
+
+
+def sdllm_compact_kv_packed(shape, k_full, v_full, idx, cache, cache_rows, stream=None) -> None:
+    if _pycall is not None and isinstance(shape, sdllm_shape_t):
+        _check(_pycall.compact_packed(_address("sdllm_compact_kv_packed"), ctypes.addressof(shape), k_full, v_full, idx, cache, cache_rows,
+                                      _stream(stream) or 0), "sdllm_compact_kv_packed")
+        return
+    _check(load().sdllm_compact_kv_packed(ctypes.byref(shape), _ptr(k_full), _ptr(v_full), _ptr(idx), _ptr(cache), cache_rows,
+                                          _stream(stream)), "sdllm_compact_kv_packed")
+
+
+def sdllm_unpack_kv(shape, cache, cache_rows, n_cached, k_out, v_out, stream=None) -> None:
+    if _pycall is not None and isinstance(shape, sdllm_shape_t):
+        _check(_pycall.unpack_kv(_address("sdllm_unpack_kv"), ctypes.addressof(shape), cache, cache_rows, n_cached, k_out, v_out,
+                                 _stream(stream) or 0), "sdllm_unpack_kv")
+        return
+    _check(load().sdllm_unpack_kv(ctypes.byref(shape), _ptr(cache), cache_rows, n_cached, _ptr(k_out), _ptr(v_out), _stream(stream)),
+           "sdllm_unpack_kv")
+
+
+def sdllm_sparse_attn_packed(shape, q_blk, cache, cache_rows, n_cached, k_blk, v_blk, out, ws, stream=None) -> None:
+    if _pycall is not None and isinstance(shape, sdllm_shape_t):
+        _check(_pycall.sparse_attn_packed(_address("sdllm_sparse_attn_packed"), ctypes.addressof(shape), q_blk, cache, cache_rows, n_cached,
+                                          k_blk, v_blk, out, ws, _stream(stream) or 0), "sdllm_sparse_attn_packed")
+        return
+    _check(load().sdllm_sparse_attn_packed(ctypes.byref(shape), _ptr(q_blk), _ptr(cache), cache_rows, n_cached, _ptr(k_blk), _ptr(v_blk),
+                                           _ptr(out), _ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0, _stream(stream)),
+           "sdllm_sparse_attn_packed")
+
+
+def sdllm_block_step_packed(shape, step_in_block, delay, q_blk, k_in, v_in, idx, cache, cache_rows, out, ws, stream=None) -> int:
+    if _pycall is not None and isinstance(shape, sdllm_shape_t):
+        state = _pycall.block_step_packed(_address("sdllm_block_step_packed"), ctypes.addressof(shape), step_in_block, delay, q_blk, k_in,
+                                          v_in, idx, cache, cache_rows, out, ws, _stream(stream) or 0)
+        if state < 0:
+            raise SdllmError(state, "sdllm_block_step_packed")
+        return state
+    st = ctypes.c_int32(-1)
+    _check(load().sdllm_block_step_packed(ctypes.byref(shape), step_in_block, delay, _ptr(q_blk), _ptr(k_in), _ptr(v_in), _ptr(idx),
+                                          _ptr(cache), cache_rows, _ptr(out), _ptr(ws),
+                                          ws.numel() * ws.element_size() if ws is not None else 0, _stream(stream), ctypes.byref(st)),
+           "sdllm_block_step_packed")
+    return st.value
+
+
+def sdllm_qk_norm_rope(shape, q_in, k_in, q_weight, k_weight, inv_freq, positions, q_out, k_out, stream=None) -> None:
+    if _pycall is not None and isinstance(shape, sdllm_qk_shape_t):
+        _check(_pycall.qk_norm_rope(_address("sdllm_qk_norm_rope"), ctypes.addressof(shape), q_in, k_in, q_weight, k_weight, inv_freq,
+                                    positions, q_out, k_out, _stream(stream) or 0), "sdllm_qk_norm_rope")
+        return
+    _check(load().sdllm_qk_norm_rope(ctypes.byref(shape), _ptr(q_in), _ptr(k_in), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
+                                     _ptr(positions), _ptr(q_out), _ptr(k_out), _stream(stream)), "sdllm_qk_norm_rope")
 
 
 def sdllm_stream_read_probe(src, sink=None, stream=None) -> None:

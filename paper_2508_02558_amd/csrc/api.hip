@@ -672,6 +672,54 @@ int32_t compact_params(const sdllm_shape_t& s, const void* k_full, const void* v
   return SDLLM_OK;
 }
 
+// ---------------------------------------------------------------- the cache of 4 bits a value
+int64_t packed_head_bytes(const sdllm_shape_t& s, int32_t cache_rows) { return (int64_t)packed_tiles(cache_rows) * packed_tile_bytes(s.head_dim); }
+
+// Launch of the attention over n_cached packed rows and the block.
+struct PackedPlan {
+  int cols, col_tiles, tiles, blk_tiles, n_split, tiles_per_split, waves;
+  size_t part_o_bytes, part_ml_bytes;
+  size_t ws_bytes() const { return part_o_bytes + part_ml_bytes; }
+};
+
+PackedPlan plan_packed(const sdllm_shape_t& s, int32_t n_cached) {
+  PackedPlan pl{};
+  pl.cols = (int)std::min<int64_t>((int64_t)(s.n_q_heads / s.n_kv_heads) * s.block_len, INT32_MAX - 31);   // beyond any launch
+  pl.col_tiles = (pl.cols + 31) / 32;
+  pl.tiles = packed_tiles(n_cached);
+  pl.blk_tiles = packed_tiles(s.block_len);
+  const int most_waves = s.dtype == SDLLM_BF16 ? kPackedWavesBf16 : kPackedWavesF32;
+  const int64_t units = (int64_t)s.batch * s.n_kv_heads * pl.col_tiles;
+  const int tiles = pl.tiles + pl.blk_tiles;
+  int n_split = (int)std::max<int64_t>(1, std::min<int64_t>(kNumCUs / units, tiles / most_waves));
+  pl.tiles_per_split = (tiles + n_split - 1) / n_split;
+  pl.n_split = (tiles + pl.tiles_per_split - 1) / pl.tiles_per_split;
+  pl.waves = std::min(most_waves, pl.tiles_per_split);
+  if (pl.n_split > 1) {
+    pl.part_o_bytes = align_up((size_t)units * pl.n_split * 32 * s.head_dim * sizeof(float));
+    pl.part_ml_bytes = align_up((size_t)units * pl.n_split * 2 * 32 * sizeof(float));
+  }
+  return pl;
+}
+
+// What a packed cache has to be, for every entry point that is given one.
+int32_t check_packed(const void* cache, int32_t cache_rows, int32_t n) {
+  if (n < 0 || cache_rows < n) return SDLLM_ERR_INVALID_ARG;
+  return n > 0 && (!cache || !aligned16(cache)) ? SDLLM_ERR_INVALID_ARG : SDLLM_OK;
+}
+
+// A wavefront for each tile and the grid in 32 bits
+int32_t fill_pack(const sdllm_shape_t& s, const void* cache, int32_t cache_rows, int32_t n, PackParams& p) {
+  p.cache = (uint8_t*)const_cast<void*>(cache);
+  p.head_bytes = packed_head_bytes(s, cache_rows);
+  p.hkv = s.n_kv_heads;
+  p.n = n;
+  p.tiles = packed_tiles(n);
+  if ((int64_t)s.batch * s.n_kv_heads * p.tiles > INT32_MAX) return SDLLM_ERR_UNSUPPORTED;
+  p.rows = s.batch * s.n_kv_heads;
+  return SDLLM_OK;
+}
+
 // Workspace of sdllm_block_step: [0, base) is shared by the attention partials and the scoring
 // buffers (used one after the other on the stream); the fused row statistics of the cache-update
 // step live behind it because they are written by the attention and read by the scoring.
@@ -704,6 +752,35 @@ BlockStepWs plan_block_step(const sdllm_shape_t& s, bool beside = true) {
   w.fuse_cols = w.fuse && fuses_columns(dense, s);
   w.stats_bytes = w.fuse ? align_up((size_t)s.batch * s.n_q_heads * row_blocks(s, s.block_len) * dense.n_split * 2 * block_rows(s.dtype) * sizeof(float)) : 0;
   return w;
+}
+
+// Workspace of sdllm_block_step_packed: that of the dense states or of the sparse one
+size_t packed_step_bytes(const sdllm_shape_t& s) {
+  return std::max({plan_block_step(s).bytes(), burst_bytes(s, s.seq_len, s.kv_stride[2], 0, 0), plan_packed(s, counts_of(s).k_total).ws_bytes()});
+}
+
+// States 0 and 1 of a block step but for the last of them, the compaction: the block's dense rows, and at an update the retained indices.
+// defer: where the merge of key splits that is left to the compaction goes (null: none is).
+int32_t dense_step(const sdllm_shape_t& s, int32_t state, const BlockStepWs& w, const void* q_blk, const void* k_in, const void* v_in,
+                   int32_t* idx, void* out, void* ws, size_t ws_bytes, hipStream_t stream, AttnParams* defer) {
+  const Counts c = counts_of(s);
+  KvSegment a{k_in, v_in, s.kv_stride[0], s.kv_stride[1], s.kv_stride[2], s.seq_len};
+  KvSegment b{nullptr, nullptr, 0, 0, 0, 0};
+  const bool update = state == SDLLM_STATE_UPDATE && c.k_total > 0;
+  int32_t st;
+  if (state == SDLLM_STATE_FULL || !w.fuse)
+    st = run_attn(s, q_blk, a, b, out, ws, ws_bytes, stream, update, nullptr, 0, 0, defer);
+  else {
+    // cache-update step: the dense attention also leaves the scoring softmax's row statistics
+    // ... and, where one workgroup owns a head, the saliency scores themselves (first buffer of the scoring workspace)
+    st = run_attn(s, q_blk, a, b, out, ws, w.base, stream, update, (float*)((char*)ws + w.base), s.block_off, candidates_resume(s),
+                  defer, w.fuse_cols ? (float*)((char*)ws + w.score_off) : nullptr, c.n_cand);
+  }
+  if (st != SDLLM_OK && defer) defer->n_split = 1;   // no partials to merge
+  if (st != SDLLM_OK || state == SDLLM_STATE_FULL) return st;
+  if (!row_stride_ok(s.q_stride, s.head_dim)) return SDLLM_ERR_INVALID_ARG;
+  return score_select_impl(s, q_blk, k_in, idx, nullptr, nullptr, (char*)ws + w.score_off, w.base - w.score_off, stream,
+                           w.fuse ? (float*)((char*)ws + w.base) : nullptr, w.stats_parts, true, w.fuse_cols);
 }
 
 }  // namespace
@@ -756,7 +833,7 @@ const char* sdllm_error_string(int32_t status) {
   }
 }
 
-int32_t sdllm_version(void) { return 100; }
+int32_t sdllm_version(void) { return 200; }
 
 int32_t sdllm_retained_count(const sdllm_shape_t* shape, int32_t* k_total, int32_t* k_pre, int32_t* k_suf) {
   const int32_t st = check_shape(shape);
@@ -791,6 +868,13 @@ int32_t sdllm_workspace_bytes(const sdllm_shape_t* shape, int32_t op, int32_t n_
     case SDLLM_OP_BLOCK_STEP:   // sdllm_block_step refuses less than the first only
       need = std::max({plan_block_step(s).bytes(), burst_bytes(s, counts_of(s).k_total, s.cache_stride[2], s.block_len, s.blk_stride[2]),
                        burst_bytes(s, s.seq_len, s.kv_stride[2], 0, 0)});
+      break;
+    case SDLLM_OP_SPARSE_ATTN_PACKED:
+      if (n_cached < 0) return SDLLM_ERR_INVALID_ARG;
+      need = plan_packed(s, n_cached).ws_bytes();
+      break;
+    case SDLLM_OP_BLOCK_STEP_PACKED:
+      need = packed_step_bytes(s);
       break;
     default: return SDLLM_ERR_INVALID_ARG;
   }
@@ -878,35 +962,153 @@ int32_t sdllm_block_step(const sdllm_shape_t* shape, int32_t step_in_block, int3
   // states 0/1: the block's rows of dense attention over all L keys of this step
   if (!row_stride_ok(s.kv_stride, s.head_dim)) return SDLLM_ERR_INVALID_ARG;
   if (state == SDLLM_STATE_UPDATE && c.k_total > 0 && (!idx || !k_cache || !v_cache)) return SDLLM_ERR_INVALID_ARG;
-  KvSegment a{k_in, v_in, s.kv_stride[0], s.kv_stride[1], s.kv_stride[2], s.seq_len};
-  KvSegment b{nullptr, nullptr, 0, 0, 0, 0};
   AttnParams pending{};           // split-KV merge still to run (cache-update step only)
   pending.n_split = 1;
-  const bool update = state == SDLLM_STATE_UPDATE && c.k_total > 0;
-  AttnParams* defer = update && w.score_off > 0 ? &pending : nullptr;
-  if (state == SDLLM_STATE_FULL || !w.fuse)
-    st = run_attn(s, q_blk, a, b, out, ws, ws_bytes, (hipStream_t)stream, update, nullptr, 0, 0, defer);
-  else {
-    // cache-update step: the dense attention also leaves the scoring softmax's row statistics
-    // ... and, where one workgroup owns a head, the saliency scores themselves (first buffer of the scoring workspace)
-    st = run_attn(s, q_blk, a, b, out, ws, w.base, (hipStream_t)stream, update, (float*)((char*)ws + w.base), s.block_off, candidates_resume(s),
-                  defer, w.fuse_cols ? (float*)((char*)ws + w.score_off) : nullptr, c.n_cand);
-  }
-  if (st != SDLLM_OK || state == SDLLM_STATE_FULL) return st;
+  AttnParams* defer = state == SDLLM_STATE_UPDATE && c.k_total > 0 && w.score_off > 0 ? &pending : nullptr;
+  st = dense_step(s, state, w, q_blk, k_in, v_in, idx, out, ws, ws_bytes, (hipStream_t)stream, defer);
+  if (state == SDLLM_STATE_FULL) return st;
   // from here on a pending merge must run whatever else fails: `out` is not complete without it
   auto finish_pending = [&](int32_t status) {
     if (pending.n_split > 1 && launch_attn_combine(pending, s.dtype, (hipStream_t)stream) != hipSuccess && status == SDLLM_OK)
       return (int32_t)SDLLM_ERR_HIP;
     return status;
   };
-  if (!row_stride_ok(s.q_stride, s.head_dim)) return finish_pending(SDLLM_ERR_INVALID_ARG);
-  st = score_select_impl(s, q_blk, k_in, idx, nullptr, nullptr, (char*)ws + w.score_off, w.base - w.score_off,
-                         (hipStream_t)stream, w.fuse ? (float*)((char*)ws + w.base) : nullptr, w.stats_parts, true, w.fuse_cols);
   if (st != SDLLM_OK) return finish_pending(st);
   if (pending.n_split == 1) return sdllm_compact_kv(shape, k_in, v_in, idx, k_cache, v_cache, stream);
   CompactParams cp{};
   if ((st = compact_params(s, k_in, v_in, idx, k_cache, v_cache, cp)) != SDLLM_OK) return finish_pending(st);
   return launch_compact_combine(cp, pending, s.dtype, (hipStream_t)stream) == hipSuccess ? SDLLM_OK : SDLLM_ERR_HIP;
+}
+
+int32_t sdllm_packed_cache_bytes(const sdllm_shape_t* shape, int32_t cache_rows, size_t* bytes) {
+  const int32_t st = check_shape(shape);
+  if (st != SDLLM_OK) return st;
+  if (!bytes || cache_rows < 0) return SDLLM_ERR_INVALID_ARG;
+  const size_t need = (size_t)shape->batch * shape->n_kv_heads * packed_head_bytes(*shape, cache_rows);
+  *bytes = need > 0 ? need : kAlign;   // never zero, so callers can always allocate
+  return SDLLM_OK;
+}
+
+int32_t sdllm_compact_kv_packed(const sdllm_shape_t* shape, const void* k_full, const void* v_full, const int32_t* idx, void* cache,
+                                int32_t cache_rows, void* stream) {
+  int32_t st = check_shape(shape);
+  if (st != SDLLM_OK) return st;
+  const sdllm_shape_t& s = *shape;
+  const int32_t n = counts_of(s).k_total;
+  if ((st = check_packed(cache, cache_rows, n)) != SDLLM_OK) return st;
+  if (n == 0) return SDLLM_OK;
+  if (!k_full || !v_full || !idx || !aligned16(k_full) || !aligned16(v_full) || !row_stride_ok(s.kv_stride, s.head_dim)) return SDLLM_ERR_INVALID_ARG;
+  PackParams p{};
+  if ((st = fill_pack(s, cache, cache_rows, n, p)) != SDLLM_OK) return st;
+  p.k = k_full; p.v = v_full; p.idx = idx;
+  p.s_sb = s.kv_stride[0]; p.s_sh = s.kv_stride[1]; p.s_sr = s.kv_stride[2];
+  return launch_pack(p, s.dtype, s.head_dim, (hipStream_t)stream) == hipSuccess ? SDLLM_OK : SDLLM_ERR_HIP;
+}
+
+int32_t sdllm_unpack_kv(const sdllm_shape_t* shape, const void* cache, int32_t cache_rows, int32_t n_cached, void* k_out, void* v_out, void* stream) {
+  int32_t st = check_shape(shape);
+  if (st != SDLLM_OK) return st;
+  const sdllm_shape_t& s = *shape;
+  if ((st = check_packed(cache, cache_rows, n_cached)) != SDLLM_OK) return st;
+  if (n_cached == 0) return SDLLM_OK;
+  if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out) || !row_stride_ok(s.cache_stride, s.head_dim)) return SDLLM_ERR_INVALID_ARG;
+  PackParams p{};
+  if ((st = fill_pack(s, cache, cache_rows, n_cached, p)) != SDLLM_OK) return st;
+  p.k_out = k_out; p.v_out = v_out;
+  p.s_sb = s.cache_stride[0]; p.s_sh = s.cache_stride[1]; p.s_sr = s.cache_stride[2];
+  return launch_unpack(p, s.dtype, s.head_dim, (hipStream_t)stream) == hipSuccess ? SDLLM_OK : SDLLM_ERR_HIP;
+}
+
+int32_t sdllm_sparse_attn_packed(const sdllm_shape_t* shape, const void* q_blk, const void* cache, int32_t cache_rows, int32_t n_cached,
+                                 const void* k_blk, const void* v_blk, void* out, void* ws, size_t ws_bytes, void* stream) {
+  int32_t st = check_shape(shape);
+  if (st != SDLLM_OK) return st;
+  const sdllm_shape_t& s = *shape;
+  if ((st = check_q(s, q_blk)) != SDLLM_OK) return st;
+  if ((st = check_packed(cache, cache_rows, n_cached)) != SDLLM_OK) return st;
+  if (!k_blk || !v_blk || !out || !aligned16(k_blk) || !aligned16(v_blk) || !aligned16(out) ||
+      !row_stride_ok(s.blk_stride, s.head_dim) || !row_stride_ok(s.out_stride, s.head_dim))
+    return SDLLM_ERR_INVALID_ARG;
+  const PackedPlan pl = plan_packed(s, n_cached);
+  // threads of one launch, merge included
+  if ((int64_t)s.batch * s.n_kv_heads * pl.col_tiles * std::max(pl.n_split * pl.waves * kWave, 32 * s.head_dim / 4) > UINT32_MAX) return SDLLM_ERR_UNSUPPORTED;
+  if (pl.n_split > 1 && (!ws || ws_bytes < pl.ws_bytes() || !aligned16(ws))) return SDLLM_ERR_WORKSPACE;
+  PackedAttnParams p{};
+  p.q = q_blk; p.out = out; p.cache = (const uint8_t*)cache; p.k_blk = k_blk; p.v_blk = v_blk;
+  p.head_bytes = packed_head_bytes(s, cache_rows);
+  p.q_sb = s.q_stride[0]; p.q_sh = s.q_stride[1]; p.q_sr = s.q_stride[2];
+  p.blk_sb = s.blk_stride[0]; p.blk_sh = s.blk_stride[1]; p.blk_sr = s.blk_stride[2];
+  p.o_sb = s.out_stride[0]; p.o_sh = s.out_stride[1]; p.o_sr = s.out_stride[2];
+  p.batch = s.batch; p.hkv = s.n_kv_heads; p.group = s.n_q_heads / s.n_kv_heads; p.nq = s.block_len;
+  p.cols = pl.cols; p.col_tiles = pl.col_tiles;
+  p.n_cached = n_cached; p.tiles = pl.tiles; p.blk_tiles = pl.blk_tiles;
+  p.scale_log2 = scale_of(s) * kLog2e;
+  p.n_split = pl.n_split; p.tiles_per_split = pl.tiles_per_split; p.waves = pl.waves;
+  p.part_o = (float*)ws; p.part_ml = (float*)((char*)ws + pl.part_o_bytes);
+  return launch_attn_packed(p, s.dtype, s.head_dim, (hipStream_t)stream) == hipSuccess ? SDLLM_OK : SDLLM_ERR_HIP;
+}
+
+int32_t sdllm_block_step_packed(const sdllm_shape_t* shape, int32_t step_in_block, int32_t delay, const void* q_blk, const void* k_in,
+                                const void* v_in, int32_t* idx, void* cache, int32_t cache_rows, void* out, void* ws, size_t ws_bytes,
+                                void* stream, int32_t* state_out) {
+  int32_t st = check_shape(shape);
+  if (st != SDLLM_OK) return st;
+  const sdllm_shape_t& s = *shape;
+  int32_t state;
+  if ((st = sdllm_cache_state(step_in_block, delay, &state)) != SDLLM_OK) return st;
+  const size_t need = std::max(packed_step_bytes(s), kAlign);
+  if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0) return SDLLM_ERR_WORKSPACE;
+  if ((st = check_q(s, q_blk)) != SDLLM_OK) return st;
+  if (!k_in || !v_in || !out || !aligned16(k_in) || !aligned16(v_in) || !aligned16(out) || !row_stride_ok(s.out_stride, s.head_dim))
+    return SDLLM_ERR_INVALID_ARG;
+  const int32_t n = counts_of(s).k_total;
+  if (state != SDLLM_STATE_FULL && (st = check_packed(cache, cache_rows, n)) != SDLLM_OK) return st;
+  if (state != SDLLM_STATE_REUSE && !row_stride_ok(s.kv_stride, s.head_dim)) return SDLLM_ERR_INVALID_ARG;
+  if (state == SDLLM_STATE_UPDATE && n > 0 && !idx) return SDLLM_ERR_INVALID_ARG;
+  if (state_out) *state_out = state;
+  if (state == SDLLM_STATE_REUSE) return sdllm_sparse_attn_packed(shape, q_blk, cache, cache_rows, n, k_in, v_in, out, ws, ws_bytes, stream);
+  st = dense_step(s, state, plan_block_step(s), q_blk, k_in, v_in, idx, out, ws, ws_bytes, (hipStream_t)stream, nullptr);
+  if (st != SDLLM_OK || state == SDLLM_STATE_FULL) return st;
+  return sdllm_compact_kv_packed(shape, k_in, v_in, idx, cache, cache_rows, stream);
+}
+
+int32_t sdllm_qk_norm_rope(const sdllm_qk_shape_t* shape, const void* q_in, const void* k_in, const void* q_weight, const void* k_weight,
+                           const float* inv_freq, const int32_t* positions, void* q_out, void* k_out, void* stream) {
+  if (!shape) return SDLLM_ERR_INVALID_ARG;
+  const sdllm_qk_shape_t& s = *shape;
+  if (s.batch < 1 || s.rows < 0 || s.n_q_heads < 0 || s.n_kv_heads < 0 || (int64_t)s.n_q_heads + s.n_kv_heads < 1 ||
+      (int64_t)s.n_q_heads + s.n_kv_heads > INT32_MAX)
+    return SDLLM_ERR_INVALID_ARG;
+  if ((s.dtype != SDLLM_BF16 && s.dtype != SDLLM_F32) || (s.norm != SDLLM_NORM_NONE && s.norm != SDLLM_NORM_RMS) ||
+      (s.pairing != SDLLM_PAIR_HALVES && s.pairing != SDLLM_PAIR_ADJACENT) || s.reserved != 0)
+    return SDLLM_ERR_INVALID_ARG;
+  if (!(s.eps >= 0.f) || !isfinite(s.eps)) return SDLLM_ERR_INVALID_ARG;
+  if (s.head_dim != 64 && s.head_dim != 128) return SDLLM_ERR_UNSUPPORTED;
+  if (s.rot_dim < 0 || s.rot_dim > s.head_dim || s.rot_dim % 2 != 0) return SDLLM_ERR_INVALID_ARG;
+  if (s.rot_dim % 16 != 0) return SDLLM_ERR_UNSUPPORTED;
+  if (s.rot_dim > 0 && !inv_freq) return SDLLM_ERR_INVALID_ARG;
+  if (s.pos_stride < 0 || (!positions && (int64_t)s.pos_begin + s.rows > (int64_t)INT32_MAX + 1)) return SDLLM_ERR_INVALID_ARG;
+  const int es = elem_size(s.dtype);
+  auto tensor_ok = [&](const void* in, const int64_t* st_in, const void* out, const int64_t* st_out, const void* weight) {
+    return in && out && aligned16(in) && aligned16(out) && aligned16(weight) && strides_ok(st_in, es) && strides_ok(st_out, es) &&
+           row_stride_ok(st_in, s.head_dim) && row_stride_ok(st_out, s.head_dim);
+  };
+  if (s.n_q_heads > 0 && !tensor_ok(q_in, s.q_in_stride, q_out, s.q_out_stride, q_weight)) return SDLLM_ERR_INVALID_ARG;
+  if (s.n_kv_heads > 0 && !tensor_ok(k_in, s.k_in_stride, k_out, s.k_out_stride, k_weight)) return SDLLM_ERR_INVALID_ARG;
+  if ((int64_t)s.batch * s.rows > INT32_MAX) return SDLLM_ERR_UNSUPPORTED;
+  if (s.rows == 0) return SDLLM_OK;
+  QkParams p{};
+  p.q_in = q_in; p.k_in = k_in; p.q_out = q_out; p.k_out = k_out;
+  p.q_weight = q_weight; p.k_weight = k_weight; p.inv_freq = inv_freq; p.positions = positions;
+  p.pos_stride = s.pos_stride; p.pos_begin = s.pos_begin;
+  p.qi_sb = s.q_in_stride[0]; p.qi_sh = s.q_in_stride[1]; p.qi_sr = s.q_in_stride[2];
+  p.ki_sb = s.k_in_stride[0]; p.ki_sh = s.k_in_stride[1]; p.ki_sr = s.k_in_stride[2];
+  p.qo_sb = s.q_out_stride[0]; p.qo_sh = s.q_out_stride[1]; p.qo_sr = s.q_out_stride[2];
+  p.ko_sb = s.k_out_stride[0]; p.ko_sh = s.k_out_stride[1]; p.ko_sr = s.k_out_stride[2];
+  p.tokens = s.batch * s.rows; p.rows = s.rows; p.hq = s.n_q_heads; p.hkv = s.n_kv_heads;
+  p.rot = s.rot_dim; p.adjacent = s.pairing == SDLLM_PAIR_ADJACENT; p.norm = s.norm == SDLLM_NORM_RMS; p.eps = s.eps;
+  p.by_rows = Divisor((uint32_t)s.rows);
+  return launch_qk_norm_rope(p, s.dtype, s.head_dim, (hipStream_t)stream) == hipSuccess ? SDLLM_OK : SDLLM_ERR_HIP;
 }
 
 int32_t sdllm_dense_attn(const sdllm_shape_t* shape, const void* q_full, const int64_t* q_full_stride,

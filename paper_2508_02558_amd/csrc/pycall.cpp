@@ -1,4 +1,4 @@
-// Calls the three entry points that a decoder makes per layer and step with tensors straight from Python.  ctypes converts fourteen
+// Calls the entry points that a decoder makes per layer with tensors straight from Python.  ctypes converts fourteen
 // arguments, eight of them fetched by a Python function each, in 2.2 us, as much as a kernel launch; this takes 0.9.  The functions
 // are given by address, so that they are those of the library that the binding has loaded.  Each returns what the entry point does;
 // block_step the state that it executed where that succeeded.
@@ -125,6 +125,90 @@ PyObject* dense_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
+PyObject* block_step_packed(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count_is(n, 13)) return nullptr;
+  Args a{args};
+  const auto f = reinterpret_cast<decltype(&sdllm_block_step_packed)>(a.address());
+  const auto* shape = static_cast<const sdllm_shape_t*>(a.address());
+  const int32_t step = (int32_t)a.number(), delay = (int32_t)a.number();
+  void *q = a.tensor(), *k = a.tensor(), *v = a.tensor(), *idx = a.tensor(), *cache = a.tensor();
+  const int32_t cache_rows = (int32_t)a.number();
+  void* out = a.tensor();
+  const size_t ws_bytes = a.bytes();
+  void *ws = a.tensor(), *stream = a.address();
+  if (!a.ok) return nullptr;
+  int32_t status, state = -1;
+  Py_BEGIN_ALLOW_THREADS
+  status = f(shape, step, delay, q, k, v, static_cast<int32_t*>(idx), cache, cache_rows, out, ws, ws_bytes, stream, &state);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status == SDLLM_OK ? state : status);
+}
+
+PyObject* sparse_attn_packed(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count_is(n, 11)) return nullptr;
+  Args a{args};
+  const auto f = reinterpret_cast<decltype(&sdllm_sparse_attn_packed)>(a.address());
+  const auto* shape = static_cast<const sdllm_shape_t*>(a.address());
+  void *q = a.tensor(), *cache = a.tensor();
+  const int32_t cache_rows = (int32_t)a.number(), n_cached = (int32_t)a.number();
+  void *kb = a.tensor(), *vb = a.tensor(), *out = a.tensor();
+  const size_t ws_bytes = a.bytes();
+  void *ws = a.tensor(), *stream = a.address();
+  if (!a.ok) return nullptr;
+  int32_t status;
+  Py_BEGIN_ALLOW_THREADS
+  status = f(shape, q, cache, cache_rows, n_cached, kb, vb, out, ws, ws_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+PyObject* compact_packed(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count_is(n, 8)) return nullptr;
+  Args a{args};
+  const auto f = reinterpret_cast<decltype(&sdllm_compact_kv_packed)>(a.address());
+  const auto* shape = static_cast<const sdllm_shape_t*>(a.address());
+  void *k = a.tensor(), *v = a.tensor(), *idx = a.tensor(), *cache = a.tensor();
+  const int32_t cache_rows = (int32_t)a.number();
+  void* stream = a.address();
+  if (!a.ok) return nullptr;
+  int32_t status;
+  Py_BEGIN_ALLOW_THREADS
+  status = f(shape, k, v, static_cast<const int32_t*>(idx), cache, cache_rows, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+PyObject* unpack_kv(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count_is(n, 8)) return nullptr;
+  Args a{args};
+  const auto f = reinterpret_cast<decltype(&sdllm_unpack_kv)>(a.address());
+  const auto* shape = static_cast<const sdllm_shape_t*>(a.address());
+  void* cache = a.tensor();
+  const int32_t cache_rows = (int32_t)a.number(), n_cached = (int32_t)a.number();
+  void *k = a.tensor(), *v = a.tensor(), *stream = a.address();
+  if (!a.ok) return nullptr;
+  int32_t status;
+  Py_BEGIN_ALLOW_THREADS
+  status = f(shape, cache, cache_rows, n_cached, k, v, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+PyObject* qk_norm_rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count_is(n, 11)) return nullptr;
+  Args a{args};
+  const auto f = reinterpret_cast<decltype(&sdllm_qk_norm_rope)>(a.address());
+  const auto* shape = static_cast<const sdllm_qk_shape_t*>(a.address());
+  void *q = a.tensor(), *k = a.tensor(), *qw = a.tensor(), *kw = a.tensor(), *freq = a.tensor(), *pos = a.tensor();
+  void *qo = a.tensor(), *ko = a.tensor(), *stream = a.address();
+  if (!a.ok) return nullptr;
+  int32_t status;
+  Py_BEGIN_ALLOW_THREADS
+  status = f(shape, q, k, qw, kw, static_cast<const float*>(freq), static_cast<const int32_t*>(pos), qo, ko, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
 template <class F>
 PyCFunction fast(F* f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
@@ -132,6 +216,11 @@ PyMethodDef methods[] = {
     {"block_step", fast(block_step), METH_FASTCALL, "function, shape, step, delay, q, k, v, idx, k_cache, v_cache, out, ws, stream"},
     {"sparse_attn", fast(sparse_attn), METH_FASTCALL, "function, shape, q, k_cache, v_cache, n_cached, k, v, out, ws, stream"},
     {"dense_attn", fast(dense_attn), METH_FASTCALL, "function, shape, q, q strides, k, v, out, out strides, stream"},
+    {"block_step_packed", fast(block_step_packed), METH_FASTCALL, "function, shape, step, delay, q, k, v, idx, cache, cache_rows, out, ws, stream"},
+    {"sparse_attn_packed", fast(sparse_attn_packed), METH_FASTCALL, "function, shape, q, cache, cache_rows, n_cached, k, v, out, ws, stream"},
+    {"compact_packed", fast(compact_packed), METH_FASTCALL, "function, shape, k, v, idx, cache, cache_rows, stream"},
+    {"unpack_kv", fast(unpack_kv), METH_FASTCALL, "function, shape, cache, cache_rows, n_cached, k, v, stream"},
+    {"qk_norm_rope", fast(qk_norm_rope), METH_FASTCALL, "function, shape, q, k, q_weight, k_weight, inv_freq, positions, q_out, k_out, stream"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

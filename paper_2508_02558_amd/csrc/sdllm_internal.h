@@ -235,4 +235,64 @@ struct DenseFullGroups { int main, tail; };
 DenseFullGroups dense_full_groups(int heads, int seq_len);
 hipError_t launch_stream_read(const void* src, size_t bytes, uint32_t* sink, hipStream_t s);
 
+// ---- the cache of 4 bits a value (packed_tile.h)
+constexpr int packed_tile_bytes(int d) { return 34 * d; }   // 32 rows of keys and values
+inline int packed_tiles(int32_t rows) { return (int)(((int64_t)rows + kTileKeys - 1) / kTileKeys); }
+
+struct PackParams {
+  const void* k;          // packing: rows that idx picks from
+  const void* v;
+  const int32_t* idx;
+  void* k_out;            // unpacking: rows written
+  void* v_out;
+  uint8_t* cache;
+  int64_t head_bytes;     // of a (batch, KV head)
+  int64_t s_sb, s_sh, s_sr;   // strides of the rows, in elements
+  int32_t rows, hkv;      // batch x KV heads, KV heads
+  int32_t n, tiles;       // rows of a (batch, KV head), tiles that hold them
+};
+
+struct PackedAttnParams {
+  const void* q;
+  void* out;
+  const uint8_t* cache;
+  const void* k_blk;
+  const void* v_blk;
+  int64_t head_bytes;
+  int64_t q_sb, q_sh, q_sr, blk_sb, blk_sh, blk_sr, o_sb, o_sh, o_sr;   // in elements
+  int32_t batch, hkv, group, nq;        // nq: rows of the block
+  int32_t cols, col_tiles;              // query rows of a KV head's group, blocks of 32 of them
+  int32_t n_cached, tiles, blk_tiles;   // tiles of the cache, of the block
+  float scale_log2;
+  int32_t n_split, tiles_per_split, waves;
+  float* part_o;                        // [batch x KV heads x col_tiles][n_split][32][d]
+  float* part_ml;                       // [batch x KV heads x col_tiles][n_split][2][32]
+};
+
+// Norm of query and key heads and rotation by position
+struct QkParams {
+  const void* q_in;
+  const void* k_in;
+  void* q_out;
+  void* k_out;
+  const void* q_weight;
+  const void* k_weight;
+  const float* inv_freq;
+  const int32_t* positions;
+  int64_t pos_stride;
+  int64_t qi_sb, qi_sh, qi_sr, ki_sb, ki_sh, ki_sr, qo_sb, qo_sh, qo_sr, ko_sb, ko_sh, ko_sr;   // in elements
+  int32_t tokens, rows, hq, hkv;        // tokens: batch x rows
+  int32_t rot, adjacent, norm, pos_begin;
+  float eps;
+  int32_t parts;                        // set by the launcher: wavefronts that share a position's heads
+  Divisor by_rows;
+};
+
+// Most wavefronts of a workgroup: with fp32 tensors the three parts of the queries take the registers of two
+constexpr int kPackedWavesBf16 = 8, kPackedWavesF32 = 4;
+hipError_t launch_pack(const PackParams& p, int dtype, int d, hipStream_t s);
+hipError_t launch_unpack(const PackParams& p, int dtype, int d, hipStream_t s);
+hipError_t launch_attn_packed(const PackedAttnParams& p, int dtype, int d, hipStream_t s);
+hipError_t launch_qk_norm_rope(const QkParams& p, int dtype, int d, hipStream_t s);
+
 }  // namespace sdllm
