@@ -688,13 +688,26 @@ PackedPlan plan_packed(const sdllm_shape_t& s, int32_t n_cached) {
   pl.col_tiles = (pl.cols + 31) / 32;
   pl.tiles = packed_tiles(n_cached);
   pl.blk_tiles = packed_tiles(s.block_len);
-  const int most_waves = s.dtype == SDLLM_BF16 ? kPackedWavesBf16 : kPackedWavesF32;
   const int64_t units = (int64_t)s.batch * s.n_kv_heads * pl.col_tiles;
-  const int tiles = pl.tiles + pl.blk_tiles;
-  int n_split = (int)std::max<int64_t>(1, std::min<int64_t>(kNumCUs / units, tiles / most_waves));
-  pl.tiles_per_split = (tiles + n_split - 1) / n_split;
-  pl.n_split = (tiles + pl.tiles_per_split - 1) / pl.tiles_per_split;
-  pl.waves = std::min(most_waves, pl.tiles_per_split);
+  const bool f32 = s.dtype == SDLLM_F32;
+  // Key splits, measured with one workgroup of up to eight wavefronts per CU (bf16, head_dim 128, 32 columns; us per call).  A tile more in a
+  // workgroup is 0.1; a split is a workgroup's fixed 7 again, in parallel, a second launch (2), and partials that are written, read and folded
+  // (0.1 and 0.014 for each unit of work, i.e. KV head and 32 columns).  The sum is least at sqrt(0.1 tiles / that): 28 units x 68 tiles
+  // 12.9 unsplit, 10.8 with 4, 11.0 with 6; 28 x 260 14.4 with 7, 15.1 with 9; 2 x 125 9.8 with 8, 11.2 with 4; 8 x 1000 17.1 with 16 to
+  // 24, 21.6 with 8; unsplit where that saves less than it costs: 32 x 20 8.2 against 9.7, 64 x 47 10.8 against 11.7 (96 x 94 16.4 against
+  // 15.2).  fp32 takes four times as long for a tile: 4 x 38 11.4 with 8, 22 unsplit, 15.3 with 4.
+  const double work = 0.1 * pl.tiles * (f32 ? 4 : 1), per_split = 0.1 + 0.014 * (double)units;
+  int n_split = std::min((int)lround(sqrt(work / per_split)), (int)(kNumCUs / units));
+  if (n_split < 2 || work * (1.0 - 1.0 / n_split) < 1.8 + per_split * n_split) n_split = 1;
+  pl.tiles_per_split = (pl.tiles + n_split - 1) / n_split;
+  pl.n_split = pl.tiles > 0 ? (pl.tiles + pl.tiles_per_split - 1) / pl.tiles_per_split : 1;
+  // Wavefronts: the fewest that take no more rounds than the most do (32 x 20 tiles and the block's 8.2 us with seven, 8.45 with eight).  With
+  // more units than CUs the LDS of four lets two workgroups share a CU, one setting up or merging while the other multiplies (512 units x 69 tiles
+  // 37.3 us, with eight wavefronts 41.1; 288 x 17 12.3, 16.8); with head_dim 64 two of eight fit.
+  int most_waves = f32 ? kPackedWavesF32 : kPackedWavesBf16;
+  if (units * pl.n_split > kNumCUs && s.head_dim == 128) most_waves = 4;
+  const int rounds = (pl.tiles_per_split + pl.blk_tiles + most_waves - 1) / most_waves;
+  pl.waves = (pl.tiles_per_split + pl.blk_tiles + rounds - 1) / rounds;
   if (pl.n_split > 1) {
     pl.part_o_bytes = align_up((size_t)units * pl.n_split * 32 * s.head_dim * sizeof(float));
     pl.part_ml_bytes = align_up((size_t)units * pl.n_split * 2 * 32 * sizeof(float));
@@ -1045,6 +1058,8 @@ int32_t sdllm_sparse_attn_packed(const sdllm_shape_t* shape, const void* q_blk, 
   p.scale_log2 = scale_of(s) * kLog2e;
   p.n_split = pl.n_split; p.tiles_per_split = pl.tiles_per_split; p.waves = pl.waves;
   p.part_o = (float*)ws; p.part_ml = (float*)((char*)ws + pl.part_o_bytes);
+  p.by_col_tiles = Divisor((uint32_t)p.col_tiles); p.by_split = Divisor((uint32_t)p.n_split);
+  p.by_hkv = Divisor((uint32_t)p.hkv); p.by_nq = Divisor((uint32_t)p.nq);
   return launch_attn_packed(p, s.dtype, s.head_dim, (hipStream_t)stream) == hipSuccess ? SDLLM_OK : SDLLM_ERR_HIP;
 }
 

@@ -264,9 +264,10 @@ struct PackedAttnParams {
   int32_t cols, col_tiles;              // query rows of a KV head's group, blocks of 32 of them
   int32_t n_cached, tiles, blk_tiles;   // tiles of the cache, of the block
   float scale_log2;
-  int32_t n_split, tiles_per_split, waves;
+  int32_t n_split, tiles_per_split, waves;   // tiles_per_split: of the cache; the block goes with the last split
   float* part_o;                        // [batch x KV heads x col_tiles][n_split][32][d]
   float* part_ml;                       // [batch x KV heads x col_tiles][n_split][2][32]
+  Divisor by_col_tiles, by_split, by_hkv, by_nq;
 };
 
 // Norm of query and key heads and rotation by position
