@@ -721,15 +721,17 @@ int32_t check_packed(const void* cache, int32_t cache_rows, int32_t n) {
   return n > 0 && (!cache || !aligned16(cache)) ? SDLLM_ERR_INVALID_ARG : SDLLM_OK;
 }
 
-// A wavefront for each tile and the grid in 32 bits
+// Two wavefronts for each tile, their threads counted in 32 bits
 int32_t fill_pack(const sdllm_shape_t& s, const void* cache, int32_t cache_rows, int32_t n, PackParams& p) {
   p.cache = (uint8_t*)const_cast<void*>(cache);
   p.head_bytes = packed_head_bytes(s, cache_rows);
   p.hkv = s.n_kv_heads;
   p.n = n;
   p.tiles = packed_tiles(n);
-  if ((int64_t)s.batch * s.n_kv_heads * p.tiles > INT32_MAX) return SDLLM_ERR_UNSUPPORTED;
+  if ((int64_t)s.batch * s.n_kv_heads * p.tiles > UINT32_MAX / (2 * kWave)) return SDLLM_ERR_UNSUPPORTED;
   p.rows = s.batch * s.n_kv_heads;
+  p.by_tiles = Divisor((uint32_t)p.tiles);
+  p.by_hkv = Divisor((uint32_t)p.hkv);
   return SDLLM_OK;
 }
 
