@@ -11,7 +11,7 @@ namespace sdllm {
 
 namespace {
 
-constexpr int kRopeThreads = 256;
+constexpr int kRopeThreads = 256;   // at most
 
 template <typename T> struct Piece;
 template <> struct Piece<__bf16> { using Vec = bf16x8; static constexpr int N = 8; };
@@ -30,7 +30,7 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(const QkPara
   constexpr int kLanes = HD / (2 * N);         // of a head
   constexpr int kHeads = kWave / kLanes;       // of a wavefront at a time
   const int lane = threadIdx.x & 63;
-  const int wave = blockIdx.x * (kRopeThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = blockIdx.x * (blockDim.x / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int token = wave / p.parts, part = wave - token * p.parts;
   if (token >= p.tokens) return;
   const int b = p.by_rows.quotient(token), row = token - b * p.rows;
@@ -126,7 +126,10 @@ hipError_t launch_as(const QkParams& q, hipStream_t s) {
   while (p.parts < passes && (int64_t)p.tokens * p.parts < 16 * kNumCUs) p.parts *= 2;
   if (p.parts > passes) p.parts = passes;
   const int64_t waves = (int64_t)p.tokens * p.parts;
-  const dim3 grid((uint32_t)((waves + 3) / 4)), block(kRopeThreads);
+  // Few wavefronts are a workgroup each, spread over all CUs (32 x 32 heads 3.33 -> 3.03 us, 666 x 16 of 64 floats 3.50 -> 3.37); many
+  // are not (8 x 4352 x 64: 205 us, 218 each for itself).
+  const int threads = waves <= 16 * kNumCUs ? kWave : kRopeThreads;
+  const dim3 grid((uint32_t)((waves * kWave + threads - 1) / threads)), block(threads);
   // Past the caches where what is written does not stay there anyway: 8 x 4352 x 64 heads, 1.14 GB, 222 -> 205 us; 666 x 16 heads of 64
   // floats, 5.5 MB, 3.5 -> 3.7.
   const int64_t bytes = (int64_t)p.tokens * (p.hq + p.hkv) * HD * sizeof(T) * 2;

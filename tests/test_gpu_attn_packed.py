@@ -164,6 +164,29 @@ def test_another_stream_and_twice_the_same():
     assert torch.equal(c.out, first)
 
 
+def test_a_cache_that_is_read_past_the_caches():
+    # 148 MB; three heads of it against the oracle, on the values that unpacking gives
+    Bt, H, n, d = 8, 32, 4250, 128
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k, v = (torch.randn(Bt, H, n, d, generator=g, device=DEV).bfloat16() for _ in range(2))
+    q, kb, vb = (torch.randn(Bt, H, 32, d, generator=g, device=DEV).bfloat16() for _ in range(3))
+    s = B.make_shape(batch=Bt, n_q_heads=H, n_kv_heads=H, head_dim=d, seq_len=n + 32, block_off=n, block_len=32, dtype=B.SDLLM_BF16, retention=1.0,
+                     kv_stride=B.strides_of(k), cache_rows=n)
+    cache = torch.empty(B.sdllm_packed_cache_bytes(s, n), dtype=torch.uint8, device=DEV)
+    assert cache.numel() > 128 << 20
+    idx = torch.arange(n, dtype=torch.int32, device=DEV).expand(Bt, H, n).contiguous()
+    B.sdllm_compact_kv_packed(s, k, v, idx, cache, n)
+    out = torch.full_like(q, float("nan"))
+    ws = torch.empty(B.sdllm_workspace_bytes(s, B.SDLLM_OP_SPARSE_ATTN_PACKED, n), dtype=torch.uint8, device=DEV)
+    B.sdllm_sparse_attn_packed(s, q, cache, n, n, kb, vb, out, ws)
+    B.sdllm_unpack_kv(s, cache, n, n, k, v)
+    torch.cuda.synchronize()
+    assert torch.isfinite(out).all()
+    for b, h in ((0, 0), (3, 17), (7, 31)):
+        one = lambda t: t[b:b + 1, h:h + 1]
+        compare(one(out), one(q), host(one(k)), host(one(v)), one(kb), one(vb), d ** -0.5, "bf16")
+
+
 def test_in_a_graph():
     c = Call(1, 8, 1, 128, 32, 3000, "bf16")
     c.run()
