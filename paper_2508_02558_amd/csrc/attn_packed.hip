@@ -302,6 +302,7 @@ struct Ring {
   static constexpr int kValueSlots = 2 * kCodes, kScaleSlots = 4 * kCodes, kBytes = 4 * kCodes + 4 * kScales;
   static constexpr int kKeyFetches = L::kLoads + 1, kValueFetches = L::kLoads, kFetches = kKeyFetches + kValueFetches;
   const uint8_t* lds;
+  uint32_t lds_at;                                       // the same as an LDS byte address, in a scalar register
   const char* tile;                                      // that is worked on
   int c, c_end, nw, lane, scale_slot;
 
@@ -311,17 +312,17 @@ struct Ring {
   __device__ __forceinline__ void fetch_keys(int parity) const {
     const char* t = tile + AHEAD * nw * L::kTile;
     const uint32_t lane16 = (uint32_t)lane * 16;
-    fetch_goes_to(lds_address(lds) + ((parity + AHEAD) & 1) * kCodes);
+    fetch_goes_to(lds_at + ((parity + AHEAD) & 1) * kCodes);
     fetch_at<L::kKeys, NT>(t, lane16);
     if constexpr (HD == 128) fetch_at<L::kKeys + 1024, NT>(t, lane16);
-    fetch_goes_to(lds_address(lds) + kScaleSlots + ((scale_slot + AHEAD) & 3) * kScales);
+    fetch_goes_to(lds_at + kScaleSlots + ((scale_slot + AHEAD) & 3) * kScales);
     if (HD == 128 || lane < 32) fetch4<NT>(t + L::kKeyScales, (uint32_t)lane * 4);
   }
   template <int AHEAD>
   __device__ __forceinline__ void fetch_values(int parity) const {
     const char* t = tile + AHEAD * nw * L::kTile + L::kValues;
     const uint32_t lane16 = (uint32_t)lane * 16;
-    fetch_goes_to(lds_address(lds) + kValueSlots + ((parity + AHEAD) & 1) * kCodes);
+    fetch_goes_to(lds_at + kValueSlots + ((parity + AHEAD) & 1) * kCodes);
     fetch_at<0, NT>(t, lane16);
     if constexpr (HD == 128) fetch_at<1024, NT>(t, lane16);
   }
@@ -421,6 +422,7 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
 
   Ring<HD, NT> ring;
   ring.lds = rest + blk_tiles * 2 * R::kBytes + wave * Ring<HD, NT>::kBytes;
+  ring.lds_at = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_address(ring.lds));
   ring.c = split * p.tiles_per_split + nw - 1 - wave;
   ring.c_end = min(p.tiles, (split + 1) * p.tiles_per_split);
   ring.tile = in_scalars((const char*)p.cache + (size_t)bg * p.head_bytes + (size_t)ring.c * L::kTile);
@@ -574,6 +576,9 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
   const bool stored = ct * kCols + m < p.cols;
   const int col = stored ? ct * kCols + m : 0, hg = p.by_nq.quotient(col), h = g * p.group + hg, row = col - hg * p.nq;
   const size_t slot = (size_t)(bg * p.col_tiles + ct) * p.n_split + split;
+  // where the lane's columns go, worked out before the barriers
+  uint64_t row_at = p.n_split == 1 ? (uint64_t)((T*)p.out + b * p.o_sb + h * p.o_sh + row * p.o_sr) : (uint64_t)(p.part_o + (slot * kCols + m) * HD);
+  asm volatile("" : "+v"(row_at));
   constexpr int kPieces = 4 * NE, kPer = 4 / NE;         // registers of a piece
   uint8_t* mine = smem + wave * park_bytes<HD>();
   __syncthreads();                                       // all wavefronts are through with what lies there
@@ -624,9 +629,9 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
         Four y;
 #pragma unroll
         for (int x = 0; x < 4; ++x) y[x] = (T)(o[x] * inv);
-        if (stored) *reinterpret_cast<Four*>((T*)p.out + b * p.o_sb + h * p.o_sh + row * p.o_sr + ch) = y;
+        if (stored) *reinterpret_cast<__attribute__((address_space(1))) Four*>(row_at + ch * sizeof(T)) = y;
       } else {
-        *reinterpret_cast<f32x4*>(p.part_o + (slot * kCols + m) * HD + ch) = o;
+        *reinterpret_cast<__attribute__((address_space(1))) f32x4*>(row_at + ch * sizeof(float)) = o;
       }
     };
     for (int u = wave; u < kPieces; u += 2 * NW) {       // the next piece is requested before this one is folded
