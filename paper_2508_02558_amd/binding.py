@@ -154,20 +154,23 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-_torch = _raw_stream = None
+_torch = _raw_stream = _device = None
 
 
 def _current_raw_stream() -> int:
     """Handle of torch's current stream on its current device.  torch.cuda.current_stream() builds a Stream object
     around the same number on every call: 3.0 us, a third of what a small step costs the host, against 0.3 us for the
-    function below it.  That one is not public, so a torch without it goes the long way."""
-    global _torch, _raw_stream
+    function below it, half of that without torch.cuda.current_device(), which looks whether torch is initialised each
+    time.  They are not public, so a torch without them goes the long way."""
+    global _torch, _raw_stream, _device
     if _torch is None:
         import torch
+        torch.cuda.current_device()                          # initialises
+        _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _torch, _raw_stream = torch, getattr(torch._C, "_cuda_getCurrentRawStream", None)
     if _raw_stream is None:
         return _torch.cuda.current_stream().cuda_stream
-    return _raw_stream(_torch.cuda.current_device())
+    return _raw_stream(_device())
 
 
 def _stream(stream) -> Optional[int]:
@@ -193,13 +196,13 @@ except ImportError:
 
 def _address(name: str) -> int:
     """Address of an entry point of the loaded library, looked up once per library."""
-    lib = load()
-    known = lib.__dict__.get("addresses")
-    if known is None:
-        known = lib.addresses = {}
-    if name not in known:
+    try:
+        return _lib.addresses[name]
+    except (AttributeError, KeyError):
+        lib = load()
+        known = lib.__dict__.setdefault("addresses", {})
         known[name] = ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
-    return known[name]
+        return known[name]
 
 
 def make_shape(*, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, seq_len: int, block_off: int,
