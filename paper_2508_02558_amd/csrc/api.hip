@@ -1112,7 +1112,8 @@ int32_t sdllm_qk_norm_rope(const sdllm_qk_shape_t* shape, const void* q_in, cons
   };
   if (s.n_q_heads > 0 && !tensor_ok(q_in, s.q_in_stride, q_out, s.q_out_stride, q_weight)) return SDLLM_ERR_INVALID_ARG;
   if (s.n_kv_heads > 0 && !tensor_ok(k_in, s.k_in_stride, k_out, s.k_out_stride, k_weight)) return SDLLM_ERR_INVALID_ARG;
-  if ((int64_t)s.batch * s.rows > UINT32_MAX / kWave) return SDLLM_ERR_UNSUPPORTED;   // a wavefront for each, its threads counted in 32 bits
+  // a wavefront for each, in workgroups of four, their threads counted in 32 bits
+  if ((int64_t)s.batch * s.rows > UINT32_MAX / kWave / 4 * 4) return SDLLM_ERR_UNSUPPORTED;
   if (s.rows == 0) return SDLLM_OK;
   QkParams p{};
   p.q_in = q_in; p.k_in = k_in; p.q_out = q_out; p.k_out = k_out;

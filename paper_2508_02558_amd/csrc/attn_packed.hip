@@ -1,13 +1,24 @@
 // Block-query attention over a cache of 4 bits a value (packed_tile.h) and the block's own keys and values (Alg. 3, cache_state == 2).
 //
 // The query rows of the heads of a KV head are one list of columns (head, row); 32 of them are a 32x32 matrix block, whatever the block length, so
-// that single tokens of grouped heads share one.  A wavefront owns 32 columns and takes tiles of 32 keys: its lanes' own bytes of the
-// tile come straight from memory (no LDS), eight codes turn into one operand of v_mfma_f32_32x32x16_bf16 by four conversions, and
+// that single tokens of grouped heads share one.  A wavefront owns 32 columns and takes tiles of 32 keys, which come through a ring in
+// LDS of its own, and makes
 //   logits^T = K_tile Q^T   (K rows as A operand: a lane holds sixteen logits of one column),
 //   O^T += V_tile^T P^T     (V codes lie in the order of those sixteen logits),
-// with the running maximum and sum of a softmax.  The numbers of the cache are bf16 numbers, so for fp32 tensors the queries and the
-// probabilities enter as the sum of three bf16 parts, all 24 bits of them: three times the products, and exact ones.
-// Keys are split over the wavefronts of a workgroup, merged through LDS, and over workgroups, whose partials a second launch folds.
+// with the running maximum and sum of a softmax.  For bf16 tensors the first product takes the codes as they lie, by the scaled matrix
+// instruction; for the second four conversions make one operand of v_mfma_f32_32x32x16_bf16 out of eight codes.  The numbers of the cache are bf16 numbers,
+// so for fp32 tensors the queries and the probabilities enter as the sum of three bf16 parts, all 24 bits of them: three times the products,
+// and exact ones.  Keys are split over the wavefronts of a workgroup, merged through LDS, and over workgroups, whose partials a second launch
+// folds.
+//
+// What bounds it.  Calls on few heads: latency; a workgroup is 5.5 us without its tiles, 2.3 of them the launch, 2 until the queries are
+// converted, 1.5 to 2 for the merge (16 KB of LDS a wavefront, in and out).  Full grids: a tile is 580 cycles of vector and 512 of matrix instructions
+// to a SIMD (measured rates: 4.5 cycles a conversion, fma or add, 8 an exponential, 32 and 64 the matrix instructions) and takes 1150 with two
+// wavefronts there; fetches held up by memory are 2 of 15 us with 224 workgroups x 73 tiles and 6 of 21 with 256 x 69 from HBM (3.9 TB/s; 18 us from
+// the memory-side cache).
+// Measured and not kept: sums and maxima between the products of the values, where the matrix unit has room for them (within 1%); a higher priority
+// for wavefronts that are there (224 x 73 -1.5%, 256 x 69 from HBM +4%); LDS for each wavefront to park its results in without waiting
+// (+1 to +4%: the code is longer); four wavefronts instead of eight (224 x 73 17.1 us in place of 14.6).
 #include "attn_merge.h"
 #include "attn_tile_math.h"
 #include "packed_tile.h"
@@ -307,6 +318,8 @@ struct Ring {
   int c, c_end, nw, lane, scale_slot;
 
   __device__ __forceinline__ bool has(int ahead) const { return c + ahead * nw < c_end; }
+  // From this tile on; past the last one it may wrap round, and is not used.
+  __device__ __forceinline__ int rows_left(int n_cached) const { return (int)((uint32_t)n_cached - (uint32_t)c * kTileKeys); }
   // AHEAD: of the tile; parity: of the tile's number among the wavefront's
   template <int AHEAD>
   __device__ __forceinline__ void fetch_keys(int parity) const {
@@ -402,7 +415,6 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
   const int pair = p.by_col_tiles.quotient(wg), ct = wg - pair * p.col_tiles;
   const int bg = p.by_split.quotient(pair), split = pair - bg * p.n_split;
   const int b = p.by_hkv.quotient(bg), g = bg - b * p.hkv;
-
 
   // The query rows, and with the last split the block's own keys and values, come once for all wavefronts, through LDS: as fragments that each
   // loads from memory they are 64 pieces of rows an instruction, 4000 cycles of the CU's address path.
@@ -546,7 +558,7 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
       ring.c += nw;
       ring.tile += nw * L::kTile;
       ring.scale_slot = (ring.scale_slot + 1) & 3;
-      m_loc = mask_max(s_next, p.n_cached - ring.c * kTileKeys, p.scale_log2, half);
+      m_loc = mask_max(s_next, ring.rows_left(p.n_cached), p.scale_log2, half);
     };
     f32x16 s0, s1;
     ring.first_keys_arrived();
@@ -559,7 +571,7 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
       queries.template logits<1>(keys, half, s0);
       queries.template logits<2>(keys, half, s0);
       queries.template logits<3>(keys, half, s0);
-      m_loc = mask_max(s0, p.n_cached - ring.c * kTileKeys, p.scale_log2, half);
+      m_loc = mask_max(s0, ring.rows_left(p.n_cached), p.scale_log2, half);
       if (wave >= blk_tiles) m_ref = fmaxf(kNoMax, fmaxf(m_loc, __shfl_xor(m_loc, 32)));   // nothing to rescale yet
     }
     while (true) {

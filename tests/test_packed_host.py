@@ -146,6 +146,13 @@ def test_norm_and_rotation_refusals(lib):
     assert call(rows=0) == B.SDLLM_OK                                    # nothing to do
 
 
+def test_norm_and_rotation_of_more_rows_than_a_launch_has_threads_for(lib):
+    # a wavefront of 64 threads for each, four to a workgroup
+    for rows in (2 ** 26 - 3, 2 ** 26, 2 ** 31 - 1):
+        shape = _qk(batch=1, rows=rows, pos_begin=0)
+        assert lib.sdllm_qk_norm_rope(ctypes.byref(shape), fake, fake, z, z, fake, fake, fake, fake, z) == B.SDLLM_ERR_UNSUPPORTED, rows
+
+
 pycall = pytest.mark.skipif(B._pycall is None, reason="built without the interpreter's headers")
 
 
