@@ -5,14 +5,14 @@
 // LDS of its own, and makes
 //   logits^T = K_tile Q^T   (K rows as A operand: a lane holds sixteen logits of one column),
 //   O^T += V_tile^T P^T     (V codes lie in the order of those sixteen logits),
-// with the running maximum and sum of a softmax.  For bf16 tensors the first product takes the codes as they lie, by the scaled matrix
-// instruction; for the second four conversions make one operand of v_mfma_f32_32x32x16_bf16 out of eight codes.  The numbers of the cache are bf16 numbers,
-// so for fp32 tensors the queries and the probabilities enter as the sum of three bf16 parts, all 24 bits of them: three times the products,
+// with the running maximum and sum of a softmax.  Four conversions make one operand of v_mfma_f32_32x32x16_bf16 out of eight codes; with more
+// than three tiles to a wavefront the first product of bf16 tensors takes the codes as they lie, by the scaled matrix instruction.  The numbers of the
+// cache are bf16 numbers, so for fp32 tensors the queries and the probabilities enter as the sum of three bf16 parts, all 24 bits of them: three times the products,
 // and exact ones.  Keys are split over the wavefronts of a workgroup, merged through LDS, and over workgroups, whose partials a second launch
 // folds.
 //
-// What bounds it.  Calls on few heads: latency; a workgroup is 5.5 us without its tiles, 2.3 of them the launch, 2 until the queries are
-// converted, 1.5 to 2 for the merge (16 KB of LDS a wavefront, in and out).  Full grids: a tile is 580 cycles of vector and 512 of matrix instructions
+// What bounds it.  Calls on few heads: latency; a workgroup is 5 us without its tiles, 2.3 of them the launch, 1.4 until the queries are
+// there (and 0.5 until they are converted), 1.5 to 2 for the merge (16 KB of LDS a wavefront, in and out).  Full grids: a tile is 580 cycles of vector and 512 of matrix instructions
 // to a SIMD (measured rates: 4.5 cycles a conversion, fma or add, 8 an exponential, 32 and 64 the matrix instructions) and takes 1150 with two
 // wavefronts there; fetches held up by memory are 2 of 15 us with 224 workgroups x 73 tiles and 6 of 21 with 256 x 69 from HBM (3.9 TB/s; 18 us from
 // the memory-side cache).
@@ -166,8 +166,9 @@ struct Operand {
 };
 
 // ---- logits of a tile of the cache
-// For fp32 tensors the codes become bf16 operands, against the three parts of the queries.
-template <typename T, int HD>
+// With the codes made into bf16 operands, against the queries' rows as they are or their three parts: for fp32 tensors, and for bf16 ones where a
+// wavefront has few tiles.
+template <typename T, int HD, bool SCALED>
 struct Queries {
   static constexpr int NF = HD / 16, PARTS = Parts<T>::N;
   bf16x8 qf[NF][PARTS];
@@ -197,13 +198,13 @@ struct Queries {
   }
 };
 
-// For bf16 tensors the codes and their scales are operands of the scaled matrix instruction as they lie in the cache, a lane's 16 bytes and
-// scale byte being 32 channels of its key.  The queries enter as two e4m3 numbers and a power of two for 32 channels: the eight bits of a bf16
+// For bf16 tensors and more tiles the codes and their scales are operands of the scaled matrix instruction as they lie in the cache, a lane's 16
+// bytes and scale byte being 32 channels of its key.  The queries enter as two e4m3 numbers and a power of two for 32 channels: the eight bits of a bf16
 // number are the four of one and the four of what is left, exactly, for magnitudes down to 2^-13 of the largest of the 32; below,
 // what is left off is under 2^-20 of that largest one.  As many cycles of the matrix unit as with bf16 operands (4 x 64 against 8 x 32 a tile), but
-// without 36 conversions a tile, a fifth of the vector instructions of the loop.
+// without 36 conversions a tile, a fifth of the vector instructions of the loop; but 0.5 us until the queries are converted and there.
 template <int HD>
-struct Queries<__bf16, HD> {
+struct Queries<__bf16, HD, true> {
   typedef __attribute__((ext_vector_type(8))) int i32x8;
   static constexpr int NI = HD / 64;
   i32x8 part[NI][2];
@@ -392,14 +393,14 @@ template <int HD> constexpr int park_bytes() { return 64 * park_row<HD>() + 64 *
 
 // LDS of a workgroup: the query rows, what the wavefronts convert of them, the rows of the block's tiles, the rings.  What is parked
 // later goes over all of it.
-template <typename T, int HD> constexpr int query_lds() { return Rows<T, HD>::kBytes + Queries<T, HD>::kShared; }
-template <typename T, int HD> constexpr int workgroup_lds(int waves, int blk_tiles) {
-  const int park = waves * park_bytes<HD>(), run = query_lds<T, HD>() + blk_tiles * 2 * Rows<T, HD>::kBytes + waves * Ring<HD, false>::kBytes;
+template <typename T, int HD, bool SCALED> constexpr int query_lds() { return Rows<T, HD>::kBytes + Queries<T, HD, SCALED>::kShared; }
+template <typename T, int HD, bool SCALED> constexpr int workgroup_lds(int waves, int blk_tiles) {
+  const int park = waves * park_bytes<HD>(), run = query_lds<T, HD, SCALED>() + blk_tiles * 2 * Rows<T, HD>::kBytes + waves * Ring<HD, false>::kBytes;
   return park > run ? park : run;
 }
-static_assert(workgroup_lds<__bf16, 128>(kPackedWavesBf16, 2) <= 160 * 1024 && workgroup_lds<float, 128>(kPackedWavesF32, 2) <= 160 * 1024, "LDS of a CU");
+static_assert(workgroup_lds<__bf16, 128, true>(kPackedWavesBf16, 2) <= 160 * 1024 && workgroup_lds<float, 128, false>(kPackedWavesF32, 2) <= 160 * 1024, "LDS of a CU");
 
-template <typename T, int HD, bool NT>
+template <typename T, int HD, bool SCALED, bool NT>
 __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(const PackedAttnParams p) {
   using L = PackedLayout<HD>;
   using R = Rows<T, HD>;
@@ -420,7 +421,8 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
   // loads from memory they are 64 pieces of rows an instruction, 4000 cycles of the CU's address path.
   // Tiles of the block are taken by the first wavefronts, which have the fewest tiles of the cache.
   const int blk_tiles = split == p.n_split - 1 ? p.blk_tiles : 0;
-  uint8_t* rest = smem + query_lds<T, HD>();
+  using Q = Queries<T, HD, SCALED>;
+  uint8_t* rest = smem + query_lds<T, HD, SCALED>();
   R::request(smem, wave, nw, lane, [&](int r) {
     const int c = min(ct * kCols + r, p.cols - 1), cg = p.by_nq.quotient(c);
     return (const T*)p.q + b * p.q_sb + (g * p.group + cg) * p.q_sh + (c - cg * p.nq) * p.q_sr;
@@ -444,7 +446,7 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
   ring.start();
   bare_barrier();
 
-  Queries<T, HD>::prepare(smem, smem + R::kBytes, wave, nw, m, half);
+  Q::prepare(smem, smem + R::kBytes, wave, nw, m, half);
 
   f32x16 acc[NE];
 #pragma unroll
@@ -509,7 +511,7 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
   }
 
   if (ring.has(0)) {
-    Queries<T, HD> queries;
+    Q queries;
     queries.load(smem, smem + R::kBytes, m, half);
     float m_loc;                                         // of the tile whose logits are there
     // One tile: its softmax and its product with the values, and the next tile's logits.  While a matrix instruction waits, for the one before
@@ -683,12 +685,12 @@ __global__ __launch_bounds__(256) void attn_packed_merge_kernel(const PackedAttn
   store_piece<T>(r, (T*)p.out + b * p.o_sb + h * p.o_sh + row * p.o_sr + c4);
 }
 
-template <typename T, int HD, bool NT>
+template <typename T, int HD, bool SCALED, bool NT>
 hipError_t launch_kernel(const PackedAttnParams& p, int units, hipStream_t s) {
   static LdsOptIn opt;
-  const hipError_t e = opt.ensure(reinterpret_cast<const void*>(attn_packed_kernel<T, HD, NT>), workgroup_lds<T, HD>(Parts<T>::kWaves, 2));
+  const hipError_t e = opt.ensure(reinterpret_cast<const void*>(attn_packed_kernel<T, HD, SCALED, NT>), workgroup_lds<T, HD, SCALED>(Parts<T>::kWaves, 2));
   if (e != hipSuccess) return e;
-  return launch(attn_packed_kernel<T, HD, NT>, dim3((uint32_t)units * p.n_split), dim3(p.waves * kWave), workgroup_lds<T, HD>(p.waves, p.blk_tiles), s, p);
+  return launch(attn_packed_kernel<T, HD, SCALED, NT>, dim3((uint32_t)units * p.n_split), dim3(p.waves * kWave), workgroup_lds<T, HD, SCALED>(p.waves, p.blk_tiles), s, p);
 }
 
 template <typename T, int HD>
@@ -699,8 +701,12 @@ hipError_t launch_as(const PackedAttnParams& p, hipStream_t s) {
   // Tiles that several blocks of columns read come from L2: 224 x 73 15.9 -> 16.7.
   const bool stream = sizeof(T) == 2 && p.col_tiles == 1 && (int64_t)units * p.tiles * PackedLayout<HD>::kTile >= (int64_t)128 << 20;
   hipError_t e;
-  if constexpr (sizeof(T) == 2) e = stream ? launch_kernel<T, HD, true>(p, units, s) : launch_kernel<T, HD, false>(p, units, s);
-  else e = launch_kernel<T, HD, false>(p, units, s);
+  if constexpr (sizeof(T) == 2) {
+    if (stream) e = launch_kernel<T, HD, true, true>(p, units, s);
+    else e = p.scaled ? launch_kernel<T, HD, true, false>(p, units, s) : launch_kernel<T, HD, false, false>(p, units, s);
+  } else {
+    e = launch_kernel<T, HD, false, false>(p, units, s);
+  }
   if (e != hipSuccess || p.n_split == 1) return e;
   return launch(attn_packed_merge_kernel<T, HD>, dim3((uint32_t)units * (kCols * HD / 4 / 256)), dim3(256), 0, s, p);
 }

@@ -234,3 +234,59 @@ def test_block_step_runs_the_states(Hq, Hkv, d, b, dtype, prompt):
     torch.cuda.synchronize()
     assert torch.equal(again, out_p)
     compare(out_p, q, want[0], want[1], kn, vn, d ** -0.5, dtype)
+
+
+# ---- heads enough that keys are not split over workgroups, and more than three tiles for each wavefront: the queries go through two 8-bit numbers
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Bt,Hq,Hkv,b,n", [(1, 64, 64, 32, 1290), (2, 64, 32, 7, 1500), (1, 260, 65, 1, 1111), (1, 128, 64, 33, 1024)])
+def test_many_tiles_for_each_wavefront(d, Bt, Hq, Hkv, b, n):
+    c = Call(Bt, Hq, Hkv, d, b, n, "bf16")
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("where", [0, 700, 1289])
+def test_one_key_of_many_tiles_takes_nearly_all(d, where):
+    def edit(k, v, c):
+        k[:, :, where] = c.q.float().cpu()[:, :, 0] * 3
+    c = Call(1, 64, 64, d, 32, 1290, "bf16", edit=edit, scale=0.5)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hkv,n", [(2, 200), (64, 1290)])
+def test_queries_with_channels_of_unlike_size_and_an_infinite_one(d, Hkv, n):
+    def edit(k, v, c):
+        c.q[:, :, :, 5] *= 64
+        c.q[:, :, :, 40:44] *= 2.0 ** -12
+        c.q[:, :, 3] *= 2.0 ** -100
+        c.q[0, 1, 6, 2] = float("inf")
+    c = Call(1, Hkv, Hkv, d, 9, n, "bf16", edit=edit, scale=0.02)
+    c.run()
+    c.q[0, 1, 6, 2] = 1.0                    # the oracle's; that row has to be NaN
+    torch.cuda.synchronize()
+    assert torch.isnan(c.out[0, 1, 6]).all()
+    again = c.out.clone()
+    c.run()
+    torch.cuda.synchronize()
+    again[0, 1, 6] = c.out[0, 1, 6]
+    assert torch.equal(again, c.out)         # and no other row has anything of it
+    c.check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_what_is_not_finite_in_many_tiles(d):
+    def edit(k, v, c):
+        k[0, 0, 1250, 3] = float("inf")      # every query of head 0
+        v[0, 1, 1270, 5] = float("nan")      # channel 5 of head 1
+        c.vb[0, 2, 1, 7] = float("inf")      # channel 7 of head 2
+    c = Call(1, 64, 64, d, 8, 1290, "bf16", edit=edit)
+    c.run()
+    torch.cuda.synchronize()
+    out = host(c.out)
+    assert np.isnan(out[0, 0]).all()
+    assert np.isnan(out[0, 1, :, 5]).all() and np.isfinite(np.delete(out[0, 1], 5, -1)).all()
+    assert np.isposinf(out[0, 2, :, 7]).all() and np.isfinite(np.delete(out[0, 2], 7, -1)).all()
+    assert np.isfinite(out[0, 3:]).all()
