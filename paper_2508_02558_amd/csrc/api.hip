@@ -1028,7 +1028,7 @@ int32_t sdllm_compact_kv_packed(const sdllm_shape_t* shape, const void* k_full, 
   if (!k_full || !v_full || !idx || !aligned16(k_full) || !aligned16(v_full) || !row_stride_ok(s.kv_stride, s.head_dim)) return SDLLM_ERR_INVALID_ARG;
   PackParams p{};
   if ((st = fill_pack(s, cache, cache_rows, n, p)) != SDLLM_OK) return st;
-  p.k = k_full; p.v = v_full; p.idx = idx;
+  p.k = k_full; p.v = v_full; p.idx = idx; p.seq_len = s.seq_len;
   p.s_sb = s.kv_stride[0]; p.s_sh = s.kv_stride[1]; p.s_sr = s.kv_stride[2];
   return launch_pack(p, s.dtype, s.head_dim, (hipStream_t)stream) == hipSuccess ? SDLLM_OK : SDLLM_ERR_HIP;
 }

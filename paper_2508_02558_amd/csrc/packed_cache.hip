@@ -34,7 +34,8 @@ __global__ __launch_bounds__(kPackThreads) void pack_kernel(const PackParams p) 
   const int row = p.by_tiles.quotient(unit), tile = unit - row * p.tiles;      // (batch, KV head), tile of it
   const int b = p.by_hkv.quotient(row), g = row - b * p.hkv;
   const int first = tile * kTileKeys, n = min(kTileKeys, p.n - first);
-  const int picked = p.idx[(size_t)row * p.n + first + min(lane & 31, n - 1)];
+  const int named = p.idx[(size_t)row * p.n + first + min(lane & 31, n - 1)];
+  const int picked = min(max(named, 0), p.seq_len - 1);   // never leave the source tensor, whatever idx holds
   const size_t base = b * p.s_sb + g * p.s_sh;
 
   if (!values) {

@@ -250,6 +250,7 @@ struct PackParams {
   int64_t s_sb, s_sh, s_sr;   // strides of the rows, in elements
   int32_t rows, hkv;      // batch x KV heads, KV heads
   int32_t n, tiles;       // rows of a (batch, KV head), tiles that hold them
+  int32_t seq_len;        // packing: rows that idx may name
   Divisor by_tiles, by_hkv;
 };
 
