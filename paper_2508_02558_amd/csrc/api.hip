@@ -678,7 +678,6 @@ int64_t packed_head_bytes(const sdllm_shape_t& s, int32_t cache_rows) { return (
 // Launch of the attention over n_cached packed rows and the block.
 struct PackedPlan {
   int cols, col_tiles, tiles, blk_tiles, n_split, tiles_per_split, waves;
-  bool scaled;
   size_t part_o_bytes, part_ml_bytes;
   size_t ws_bytes() const { return part_o_bytes + part_ml_bytes; }
 };
@@ -717,10 +716,6 @@ PackedPlan plan_packed(const sdllm_shape_t& s, int32_t n_cached) {
   if (units * pl.n_split > kNumCUs && s.head_dim == 128) most_waves = 4;
   const int rounds = (pl.tiles_per_split + pl.blk_tiles + most_waves - 1) / most_waves;
   pl.waves = (pl.tiles_per_split + pl.blk_tiles + rounds - 1) / rounds;
-  // Converting the queries for the scaled matrix instruction pays from four rounds on (us with and without; bf16): nothing cached 7.6 / 6.1,
-  // 32 units x 1 tile 6.0 / 5.3, 32 x 7 6.3 / 6.0, three rounds 8.0 / 8.0, four 8.8 / 8.9, 224 x 32 10.7 / 11.1, 256 x 68 18.4 / 19.5; head_dim 64 likewise
-  // (32 x 11 7.5 / 7.35, 256 x 68 12.2 / 12.8).
-  pl.scaled = rounds > 3;
   if (pl.n_split > 1) {
     pl.part_o_bytes = align_up((size_t)units * pl.n_split * 32 * s.head_dim * sizeof(float));
     pl.part_ml_bytes = align_up((size_t)units * pl.n_split * 2 * 32 * sizeof(float));
@@ -1071,7 +1066,7 @@ int32_t sdllm_sparse_attn_packed(const sdllm_shape_t* shape, const void* q_blk, 
   p.cols = pl.cols; p.col_tiles = pl.col_tiles;
   p.n_cached = n_cached; p.tiles = pl.tiles; p.blk_tiles = pl.blk_tiles;
   p.scale_log2 = scale_of(s) * kLog2e;
-  p.n_split = pl.n_split; p.tiles_per_split = pl.tiles_per_split; p.waves = pl.waves; p.scaled = pl.scaled;
+  p.n_split = pl.n_split; p.tiles_per_split = pl.tiles_per_split; p.waves = pl.waves;
   p.part_o = (float*)ws; p.part_ml = (float*)((char*)ws + pl.part_o_bytes);
   p.by_col_tiles = Divisor((uint32_t)p.col_tiles); p.by_split = Divisor((uint32_t)p.n_split);
   p.by_hkv = Divisor((uint32_t)p.hkv); p.by_nq = Divisor((uint32_t)p.nq);

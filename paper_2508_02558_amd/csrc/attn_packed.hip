@@ -5,14 +5,13 @@
 // LDS of its own, and makes
 //   logits^T = K_tile Q^T   (K rows as A operand: a lane holds sixteen logits of one column),
 //   O^T += V_tile^T P^T     (V codes lie in the order of those sixteen logits),
-// with the running maximum and sum of a softmax.  Four conversions make one operand of v_mfma_f32_32x32x16_bf16 out of eight codes; with more
-// than three tiles to a wavefront the first product of bf16 tensors takes the codes as they lie, by the scaled matrix instruction.  The numbers of the
+// with the running maximum and sum of a softmax.  Four conversions make one operand of v_mfma_f32_32x32x16_bf16 out of eight codes.  The numbers of the
 // cache are bf16 numbers, so for fp32 tensors the queries and the probabilities enter as the sum of three bf16 parts, all 24 bits of them: three times the products,
 // and exact ones.  Keys are split over the wavefronts of a workgroup, merged through LDS, and over workgroups, whose partials a second launch
 // folds.
 //
 // What bounds it.  Calls on few heads: latency; a workgroup is 5 us without its tiles, 2.3 of them the launch, 1.4 until the queries are
-// there (and 0.5 until they are converted), 1.5 to 2 for the merge (16 KB of LDS a wavefront, in and out).  Full grids: a tile is 580 cycles of vector and 512 of matrix instructions
+// there, 1.5 to 2 for the merge (16 KB of LDS a wavefront, in and out).  Full grids: a tile is 580 cycles of vector and 512 of matrix instructions
 // to a SIMD (measured rates: 4.5 cycles a conversion, fma or add, 8 an exponential, 32 and 64 the matrix instructions) and takes 1150 with two
 // wavefronts there; fetches held up by memory are 2 of 15 us with 224 workgroups x 73 tiles and 6 of 21 with 256 x 69 from HBM (3.9 TB/s; 18 us from
 // the memory-side cache).
@@ -166,16 +165,15 @@ struct Operand {
 };
 
 // ---- logits of a tile of the cache
-// With the codes made into bf16 operands, against the queries' rows as they are or their three parts: for fp32 tensors, and for bf16 ones where a
-// wavefront has few tiles.
-template <typename T, int HD, bool SCALED>
+// The codes are made into bf16 operands, against the queries' rows as they are or their three parts.  The scaled matrix instruction takes codes as
+// they lie and would save the conversions, but its other operand has eight bits a number, and two such numbers for a query leave off what
+// is below 2^-13 of the largest of 32 channels.
+template <typename T, int HD>
 struct Queries {
   static constexpr int NF = HD / 16, PARTS = Parts<T>::N;
   bf16x8 qf[NF][PARTS];
 
-  static constexpr int kShared = 0;
-  static __device__ __forceinline__ void prepare(const uint8_t*, uint8_t*, int, int, int, int) {}
-  __device__ __forceinline__ void load(const uint8_t* rows, const uint8_t*, int m, int half) {
+  __device__ __forceinline__ void load(const uint8_t* rows, int m, int half) {
 #pragma unroll
     for (int f = 0; f < NF; ++f) lds_load8<T, HD>(rows, m, 32 * (2 * (f >> 2) + half) + 8 * (f & 3), qf[f]);
   }
@@ -194,96 +192,6 @@ struct Queries {
 #pragma unroll
         for (int n = PARTS - 1; n >= 0; --n) s = mfma(kf, qf[4 * STEP + st][n], s);
       }
-    }
-  }
-};
-
-// For bf16 tensors and more tiles the codes and their scales are operands of the scaled matrix instruction as they lie in the cache, a lane's 16
-// bytes and scale byte being 32 channels of its key.  The queries enter as two e4m3 numbers and a power of two for 32 channels: the eight bits of a bf16
-// number are the four of one and the four of what is left, exactly, for magnitudes down to 2^-13 of the largest of the 32; below,
-// what is left off is under 2^-20 of that largest one.  As many cycles of the matrix unit as with bf16 operands (4 x 64 against 8 x 32 a tile), but
-// without 36 conversions a tile, a fifth of the vector instructions of the loop; but 0.5 us until the queries are converted and there.
-template <int HD>
-struct Queries<__bf16, HD, true> {
-  typedef __attribute__((ext_vector_type(8))) int i32x8;
-  static constexpr int NI = HD / 64;
-  i32x8 part[NI][2];
-  uint32_t scales;                                       // bytes 2 i + part
-
-  // What the wavefronts convert for each other, [group of 32 channels: 2 NI][part][64 lanes] x 16 bytes, and the scale bytes, [lane][part] per i
-  static constexpr int kShared = 2 * NI * 2 * 1024 + NI * 64 * 2;
-  static __device__ __forceinline__ void convert(const uint8_t* rows, uint8_t* shared, int group, int m, int half) {
-    typedef __attribute__((ext_vector_type(2))) short i16x2;
-    // a lane's operand holds sixteen channels of either group of a step, its half of them; its scale is that of the group of its half
-    u32x4 x[2];
-    uint32_t top = 0;                                    // of the magnitudes, as bits of floats
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      x[st] = *reinterpret_cast<const u32x4*>(Rows<__bf16, HD>::place(rows, m, (32 * group + 16 * half + 8 * st) * 2));
-#pragma unroll
-      for (int c = 0; c < 4; ++c) top = max(top, max(x[st][c] & 0x7fff0000u, x[st][c] << 16 & 0x7fff0000u));
-    }
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-    // the largest becomes 128 to 256; an infinity or NaN makes the column NaN
-    const uint32_t byte = top >= 0x7f800000u ? 255 : (uint32_t)max((int)(top >> 23) - 7, 5), fine_byte = byte == 255 ? 255 : byte - 4;
-    const float scale = __builtin_bit_cast(float, byte << 23), finer = __builtin_bit_cast(float, fine_byte << 23);
-    u32x4 hi4, lo4;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      float v[4];
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const uint32_t two = x[w >> 1][2 * (w & 1) + c];
-        v[2 * c] = __builtin_bit_cast(float, two << 16);
-        v[2 * c + 1] = __builtin_bit_cast(float, two & 0xffff0000u);
-      }
-      i16x2 hi = {0, 0}, lo = {0, 0};
-      hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, v[0], v[1], scale, false);
-      hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, v[2], v[3], scale, true);
-      const int word = __builtin_bit_cast(int, hi);
-      const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, scale, false);
-      const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, scale, true);
-      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, v[0] - a[0], v[1] - a[1], finer, false);
-      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, v[2] - b[0], v[3] - b[1], finer, true);
-      hi4[w] = (uint32_t)word;
-      lo4[w] = __builtin_bit_cast(uint32_t, lo);
-    }
-    const int lane = half * 32 + m;
-    reinterpret_cast<u32x4*>(shared)[(2 * group) * 64 + lane] = hi4;
-    reinterpret_cast<u32x4*>(shared)[(2 * group + 1) * 64 + lane] = lo4;
-    if (half == (group & 1)) *reinterpret_cast<uint16_t*>(shared + 2 * NI * 2 * 1024 + ((group >> 1) * 64 + lane) * 2) = (uint16_t)(byte | fine_byte << 8);
-  }
-  // Before a barrier, and after it
-  static __device__ __forceinline__ void prepare(const uint8_t* rows, uint8_t* shared, int wave, int nw, int m, int half) {
-    for (int group = wave; group < 2 * NI; group += nw) convert(rows, shared, group, m, half);
-    __syncthreads();
-  }
-  __device__ __forceinline__ void load(const uint8_t*, const uint8_t* shared, int m, int half) {
-    const int lane = half * 32 + m;
-    scales = 0;
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-#pragma unroll
-      for (int which = 0; which < 2; ++which) {
-        const u32x4 a = reinterpret_cast<const u32x4*>(shared)[(4 * i + which) * 64 + lane], b = reinterpret_cast<const u32x4*>(shared)[(4 * i + 2 + which) * 64 + lane];
-        part[i][which] = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
-      }
-      scales |= (uint32_t)*reinterpret_cast<const uint16_t*>(shared + 2 * NI * 2 * 1024 + (i * 64 + lane) * 2) << (16 * i);
-    }
-  }
-  template <int STEP>
-  __device__ __forceinline__ void logits(const Operand<HD>& keys, int half, f32x16& s) const {
-    constexpr int kFp4 = 4, kFp8 = 0;
-    if constexpr (STEP == 0) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-    }
-    // the finer parts first
-    constexpr int i = NI == 2 ? STEP & 1 : 0, which = NI == 2 ? 1 - (STEP >> 1) : 1 - STEP;
-    if constexpr (STEP < 2 * NI) {
-      const i32x8 codes = {(int)keys.codes[i][0], (int)keys.codes[i][1], (int)keys.codes[i][2], (int)keys.codes[i][3], 0, 0, 0, 0};
-      s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes, part[i][which], s, kFp4, kFp8, 2 * i, (int)(keys.scales >> (8 * half)), 2 * i + which,
-                                                          (int)scales);
     }
   }
 };
@@ -391,16 +299,14 @@ static_assert(PackedLayout<128>::kKeyScales + 128 == PackedLayout<128>::kValueSc
 template <int HD> constexpr int park_row() { return 16 * (HD / 32) * 4 + 16; }
 template <int HD> constexpr int park_bytes() { return 64 * park_row<HD>() + 64 * 4; }
 
-// LDS of a workgroup: the query rows, what the wavefronts convert of them, the rows of the block's tiles, the rings.  What is parked
-// later goes over all of it.
-template <typename T, int HD, bool SCALED> constexpr int query_lds() { return Rows<T, HD>::kBytes + Queries<T, HD, SCALED>::kShared; }
-template <typename T, int HD, bool SCALED> constexpr int workgroup_lds(int waves, int blk_tiles) {
-  const int park = waves * park_bytes<HD>(), run = query_lds<T, HD, SCALED>() + blk_tiles * 2 * Rows<T, HD>::kBytes + waves * Ring<HD, false>::kBytes;
+// LDS of a workgroup: the query rows, the rows of the block's tiles, the rings.  What is parked later goes over all of it.
+template <typename T, int HD> constexpr int workgroup_lds(int waves, int blk_tiles) {
+  const int park = waves * park_bytes<HD>(), run = (1 + 2 * blk_tiles) * Rows<T, HD>::kBytes + waves * Ring<HD, false>::kBytes;
   return park > run ? park : run;
 }
-static_assert(workgroup_lds<__bf16, 128, true>(kPackedWavesBf16, 2) <= 160 * 1024 && workgroup_lds<float, 128, false>(kPackedWavesF32, 2) <= 160 * 1024, "LDS of a CU");
+static_assert(workgroup_lds<__bf16, 128>(kPackedWavesBf16, 2) <= 160 * 1024 && workgroup_lds<float, 128>(kPackedWavesF32, 2) <= 160 * 1024, "LDS of a CU");
 
-template <typename T, int HD, bool SCALED, bool NT>
+template <typename T, int HD, bool NT>
 __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(const PackedAttnParams p) {
   using L = PackedLayout<HD>;
   using R = Rows<T, HD>;
@@ -421,8 +327,7 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
   // loads from memory they are 64 pieces of rows an instruction, 4000 cycles of the CU's address path.
   // Tiles of the block are taken by the first wavefronts, which have the fewest tiles of the cache.
   const int blk_tiles = split == p.n_split - 1 ? p.blk_tiles : 0;
-  using Q = Queries<T, HD, SCALED>;
-  uint8_t* rest = smem + query_lds<T, HD, SCALED>();
+  uint8_t* rest = smem + R::kBytes;
   R::request(smem, wave, nw, lane, [&](int r) {
     const int c = min(ct * kCols + r, p.cols - 1), cg = p.by_nq.quotient(c);
     return (const T*)p.q + b * p.q_sb + (g * p.group + cg) * p.q_sh + (c - cg * p.nq) * p.q_sr;
@@ -445,8 +350,6 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
   ring.scale_slot = 0;
   ring.start();
   bare_barrier();
-
-  Q::prepare(smem, smem + R::kBytes, wave, nw, m, half);
 
   f32x16 acc[NE];
 #pragma unroll
@@ -511,8 +414,8 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
   }
 
   if (ring.has(0)) {
-    Q queries;
-    queries.load(smem, smem + R::kBytes, m, half);
+    Queries<T, HD> queries;
+    queries.load(smem, m, half);
     float m_loc;                                         // of the tile whose logits are there
     // One tile: its softmax and its product with the values, and the next tile's logits.  While a matrix instruction waits, for the one before
     // it or for the unit, nothing of any wavefront is issued to the SIMD's vector units; so each is followed by as many vector instructions as
@@ -685,12 +588,12 @@ __global__ __launch_bounds__(256) void attn_packed_merge_kernel(const PackedAttn
   store_piece<T>(r, (T*)p.out + b * p.o_sb + h * p.o_sh + row * p.o_sr + c4);
 }
 
-template <typename T, int HD, bool SCALED, bool NT>
+template <typename T, int HD, bool NT>
 hipError_t launch_kernel(const PackedAttnParams& p, int units, hipStream_t s) {
   static LdsOptIn opt;
-  const hipError_t e = opt.ensure(reinterpret_cast<const void*>(attn_packed_kernel<T, HD, SCALED, NT>), workgroup_lds<T, HD, SCALED>(Parts<T>::kWaves, 2));
+  const hipError_t e = opt.ensure(reinterpret_cast<const void*>(attn_packed_kernel<T, HD, NT>), workgroup_lds<T, HD>(Parts<T>::kWaves, 2));
   if (e != hipSuccess) return e;
-  return launch(attn_packed_kernel<T, HD, SCALED, NT>, dim3((uint32_t)units * p.n_split), dim3(p.waves * kWave), workgroup_lds<T, HD, SCALED>(p.waves, p.blk_tiles), s, p);
+  return launch(attn_packed_kernel<T, HD, NT>, dim3((uint32_t)units * p.n_split), dim3(p.waves * kWave), workgroup_lds<T, HD>(p.waves, p.blk_tiles), s, p);
 }
 
 template <typename T, int HD>
@@ -701,12 +604,8 @@ hipError_t launch_as(const PackedAttnParams& p, hipStream_t s) {
   // Tiles that several blocks of columns read come from L2: 224 x 73 15.9 -> 16.7.
   const bool stream = sizeof(T) == 2 && p.col_tiles == 1 && (int64_t)units * p.tiles * PackedLayout<HD>::kTile >= (int64_t)128 << 20;
   hipError_t e;
-  if constexpr (sizeof(T) == 2) {
-    if (stream) e = launch_kernel<T, HD, true, true>(p, units, s);
-    else e = p.scaled ? launch_kernel<T, HD, true, false>(p, units, s) : launch_kernel<T, HD, false, false>(p, units, s);
-  } else {
-    e = launch_kernel<T, HD, false, false>(p, units, s);
-  }
+  if constexpr (sizeof(T) == 2) e = stream ? launch_kernel<T, HD, true>(p, units, s) : launch_kernel<T, HD, false>(p, units, s);
+  else e = launch_kernel<T, HD, false>(p, units, s);
   if (e != hipSuccess || p.n_split == 1) return e;
   return launch(attn_packed_merge_kernel<T, HD>, dim3((uint32_t)units * (kCols * HD / 4 / 256)), dim3(256), 0, s, p);
 }
