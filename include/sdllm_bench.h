@@ -56,6 +56,16 @@ int32_t sdllm_launch_plan(const sdllm_shape_t* shape, int32_t call, int32_t n_ca
  * Host only. */
 int32_t sdllm_burst_splits(const sdllm_shape_t* shape, int32_t call, int32_t n_cached, int32_t* splits);
 
+typedef struct sdllm_packed_plan {
+  int32_t key_splits;  /* workgroups that share the keys of a KV head and 32 of its query rows; merged by a second launch if more than one */
+  int32_t waves;       /* per workgroup */
+  int32_t rounds;      /* most tiles of a wavefront, the block's among them */
+  int32_t past_caches; /* 1 if the cache is read with loads that leave nothing in the caches */
+} sdllm_packed_plan_t;
+
+/* How sdllm_sparse_attn_packed of this shape over n_cached rows, or state 2 of sdllm_block_step_packed, is launched.  Host only. */
+int32_t sdllm_packed_plan(const sdllm_shape_t* shape, int32_t n_cached, sdllm_packed_plan_t* plan);
+
 /* SDLLM_CALL_DENSE on SDLLM_KERNEL_DENSE: *groups is the key groups of the launch that the workgroups of a last, small round are, 0 for a
  * call (or a shape) without such a launch.  Host only. */
 int32_t sdllm_dense_tail_groups(const sdllm_shape_t* shape, int32_t* groups);

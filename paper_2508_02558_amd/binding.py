@@ -35,7 +35,7 @@ EXPORTED = ("sdllm_error_string", "sdllm_version", "sdllm_retained_count", "sdll
             "sdllm_sparse_attn_noalloc", "sdllm_block_step", "sdllm_dense_attn", "sdllm_packed_cache_bytes",
             "sdllm_compact_kv_packed", "sdllm_unpack_kv", "sdllm_sparse_attn_packed", "sdllm_block_step_packed",
             "sdllm_qk_norm_rope", "sdllm_stream_read_probe",
-            "sdllm_launch_plan", "sdllm_burst_splits", "sdllm_dense_tail_groups",
+            "sdllm_launch_plan", "sdllm_packed_plan", "sdllm_burst_splits", "sdllm_dense_tail_groups",
             "sdllm_column_kernel")
 
 # constants of include/sdllm_bench.h
@@ -70,6 +70,10 @@ class sdllm_qk_shape_t(ctypes.Structure):
 class sdllm_launch_plan_t(ctypes.Structure):
     _fields_ = [("kernel", ctypes.c_int32), ("key_splits", ctypes.c_int32), ("waves", ctypes.c_int32),
                 ("touches_ahead", ctypes.c_int32), ("key_groups", ctypes.c_int32)]
+
+
+class sdllm_packed_plan_t(ctypes.Structure):
+    _fields_ = [("key_splits", ctypes.c_int32), ("waves", ctypes.c_int32), ("rounds", ctypes.c_int32), ("past_caches", ctypes.c_int32)]
 
 
 class SdllmError(RuntimeError):
@@ -131,6 +135,8 @@ def load() -> ctypes.CDLL:
     lib.sdllm_stream_read_probe.argtypes = [vp, sz, vp, vp]
     lib.sdllm_launch_plan.restype = i32
     lib.sdllm_launch_plan.argtypes = [shp, i32, i32, ctypes.POINTER(sdllm_launch_plan_t)]
+    lib.sdllm_packed_plan.restype = i32
+    lib.sdllm_packed_plan.argtypes = [shp, i32, ctypes.POINTER(sdllm_packed_plan_t)]
     lib.sdllm_burst_splits.restype = i32
     lib.sdllm_burst_splits.argtypes = [shp, i32, i32, i32p]
     lib.sdllm_dense_tail_groups.restype = i32
@@ -397,6 +403,12 @@ def sdllm_stream_read_probe(src, sink=None, stream=None) -> None:
 def sdllm_launch_plan(shape: sdllm_shape_t, call: int, n_cached: int = 0) -> sdllm_launch_plan_t:
     plan = sdllm_launch_plan_t()
     _check(load().sdllm_launch_plan(ctypes.byref(shape), call, n_cached, ctypes.byref(plan)), "sdllm_launch_plan")
+    return plan
+
+
+def sdllm_packed_plan(shape: sdllm_shape_t, n_cached: int) -> sdllm_packed_plan_t:
+    plan = sdllm_packed_plan_t()
+    _check(load().sdllm_packed_plan(ctypes.byref(shape), n_cached, ctypes.byref(plan)), "sdllm_packed_plan")
     return plan
 
 

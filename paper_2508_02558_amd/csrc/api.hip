@@ -678,6 +678,7 @@ int64_t packed_head_bytes(const sdllm_shape_t& s, int32_t cache_rows) { return (
 // Launch of the attention over n_cached packed rows and the block.
 struct PackedPlan {
   int cols, col_tiles, tiles, blk_tiles, n_split, tiles_per_split, waves;
+  bool past_caches;
   size_t part_o_bytes, part_ml_bytes;
   size_t ws_bytes() const { return part_o_bytes + part_ml_bytes; }
 };
@@ -716,6 +717,10 @@ PackedPlan plan_packed(const sdllm_shape_t& s, int32_t n_cached) {
   if (units * pl.n_split > kNumCUs && s.head_dim == 128) most_waves = 4;
   const int rounds = (pl.tiles_per_split + pl.blk_tiles + most_waves - 1) / most_waves;
   pl.waves = (pl.tiles_per_split + pl.blk_tiles + rounds - 1) / rounds;
+  // Past the caches where every tile is read once and two such calls would not fit the memory-side cache (256 MB) together: 512 units x 69
+  // tiles, 150 MB, 37.6 -> 34.5 us, 256 x 69, 75 MB, 22.0 -> 20.5 us with 900 MB of other caches read in between, but 18.6 -> 20.5 with 150 MB.
+  // Tiles that several blocks of columns read come from L2: 224 x 73 15.9 -> 16.7.
+  pl.past_caches = !f32 && pl.col_tiles == 1 && units * pl.tiles * packed_tile_bytes(s.head_dim) >= (int64_t)128 << 20;
   if (pl.n_split > 1) {
     pl.part_o_bytes = align_up((size_t)units * pl.n_split * 32 * s.head_dim * sizeof(float));
     pl.part_ml_bytes = align_up((size_t)units * pl.n_split * 2 * 32 * sizeof(float));
@@ -1066,7 +1071,7 @@ int32_t sdllm_sparse_attn_packed(const sdllm_shape_t* shape, const void* q_blk, 
   p.cols = pl.cols; p.col_tiles = pl.col_tiles;
   p.n_cached = n_cached; p.tiles = pl.tiles; p.blk_tiles = pl.blk_tiles;
   p.scale_log2 = scale_of(s) * kLog2e;
-  p.n_split = pl.n_split; p.tiles_per_split = pl.tiles_per_split; p.waves = pl.waves;
+  p.n_split = pl.n_split; p.tiles_per_split = pl.tiles_per_split; p.waves = pl.waves; p.past_caches = pl.past_caches;
   p.part_o = (float*)ws; p.part_ml = (float*)((char*)ws + pl.part_o_bytes);
   p.by_col_tiles = Divisor((uint32_t)p.col_tiles); p.by_split = Divisor((uint32_t)p.n_split);
   p.by_hkv = Divisor((uint32_t)p.hkv); p.by_nq = Divisor((uint32_t)p.nq);
@@ -1200,6 +1205,16 @@ int32_t sdllm_launch_plan(const sdllm_shape_t* shape, int32_t call, int32_t n_ca
   plan->key_splits = pl.n_split;
   plan->waves = pl.waves;
   plan->touches_ahead = pl.stream && stream_touches_ahead(s.n_q_heads / s.n_kv_heads, pl.tiles_per_split, pl.waves);
+  return SDLLM_OK;
+}
+
+int32_t sdllm_packed_plan(const sdllm_shape_t* shape, int32_t n_cached, sdllm_packed_plan_t* plan) {
+  const int32_t st = check_shape(shape);
+  if (st != SDLLM_OK) return st;
+  if (!plan || n_cached < 0) return SDLLM_ERR_INVALID_ARG;
+  const PackedPlan pl = plan_packed(*shape, n_cached);
+  const int tiles = pl.tiles_per_split + pl.blk_tiles;
+  *plan = sdllm_packed_plan_t{pl.n_split, pl.waves, (tiles + pl.waves - 1) / pl.waves, pl.past_caches};
   return SDLLM_OK;
 }
 

@@ -599,12 +599,8 @@ hipError_t launch_kernel(const PackedAttnParams& p, int units, hipStream_t s) {
 template <typename T, int HD>
 hipError_t launch_as(const PackedAttnParams& p, hipStream_t s) {
   const int units = p.batch * p.hkv * p.col_tiles;
-  // Past the caches where every tile is read once and two such calls would not fit the memory-side cache (256 MB) together: 512 units x 69
-  // tiles, 150 MB, 37.6 -> 34.5 us, 256 x 69, 75 MB, 22.0 -> 20.5 us with 900 MB of other caches read in between, but 18.6 -> 20.5 with 150 MB.
-  // Tiles that several blocks of columns read come from L2: 224 x 73 15.9 -> 16.7.
-  const bool stream = sizeof(T) == 2 && p.col_tiles == 1 && (int64_t)units * p.tiles * PackedLayout<HD>::kTile >= (int64_t)128 << 20;
   hipError_t e;
-  if constexpr (sizeof(T) == 2) e = stream ? launch_kernel<T, HD, true>(p, units, s) : launch_kernel<T, HD, false>(p, units, s);
+  if constexpr (sizeof(T) == 2) e = p.past_caches ? launch_kernel<T, HD, true>(p, units, s) : launch_kernel<T, HD, false>(p, units, s);
   else e = launch_kernel<T, HD, false>(p, units, s);
   if (e != hipSuccess || p.n_split == 1) return e;
   return launch(attn_packed_merge_kernel<T, HD>, dim3((uint32_t)units * (kCols * HD / 4 / 256)), dim3(256), 0, s, p);

@@ -267,6 +267,7 @@ struct PackedAttnParams {
   int32_t n_cached, tiles, blk_tiles;   // tiles of the cache, of the block
   float scale_log2;
   int32_t n_split, tiles_per_split, waves;   // tiles_per_split: of the cache; the block goes with the last split
+  int32_t past_caches;                  // tiles are read past the caches (bf16)
   float* part_o;                        // [batch x KV heads x col_tiles][n_split][32][d]
   float* part_ml;                       // [batch x KV heads x col_tiles][n_split][2][32]
   Divisor by_col_tiles, by_split, by_hkv, by_nq;
