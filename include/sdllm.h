@@ -241,6 +241,8 @@ int32_t sdllm_dense_attn(const sdllm_shape_t* shape, const void* q_full, const i
  *   d bytes       key scales   [32 rows][d/32 groups]: e + 127, or 255 for NaN
  *   d bytes       value scales [d channels]
  * Rows past those written of the last tile hold zeros.
+ *
+ * These operations refuse shapes of 2^31 query heads or more in all (batch x n_q_heads), and caches of 2^63 bytes or more: SDLLM_ERR_UNSUPPORTED.
  */
 
 /* Bytes of a packed cache for cache_rows >= 0 rows per (batch, KV head).  Reads batch, n_kv_heads and head_dim of `shape`.  Host call. */

@@ -673,6 +673,14 @@ int32_t compact_params(const sdllm_shape_t& s, const void* k_full, const void* v
 }
 
 // ---------------------------------------------------------------- the cache of 4 bits a value
+// Heads in all are counted in 32 bits.
+bool heads_fit(const sdllm_shape_t& s) { return (int64_t)s.batch * s.n_q_heads <= INT32_MAX; }
+
+int32_t check_packed_shape(const sdllm_shape_t* s) {
+  const int32_t st = check_shape(s);
+  return st == SDLLM_OK && !heads_fit(*s) ? SDLLM_ERR_UNSUPPORTED : st;
+}
+
 int64_t packed_head_bytes(const sdllm_shape_t& s, int32_t cache_rows) { return (int64_t)packed_tiles(cache_rows) * packed_tile_bytes(s.head_dim); }
 
 // Launch of the attention over n_cached packed rows and the block.
@@ -720,7 +728,7 @@ PackedPlan plan_packed(const sdllm_shape_t& s, int32_t n_cached) {
   // Past the caches where every tile is read once and two such calls would not fit the memory-side cache (256 MB) together: 512 units x 69
   // tiles, 150 MB, 37.6 -> 34.5 us, 256 x 69, 75 MB, 22.0 -> 20.5 us with 900 MB of other caches read in between, but 18.6 -> 20.5 with 150 MB.
   // Tiles that several blocks of columns read come from L2: 224 x 73 15.9 -> 16.7.
-  pl.past_caches = !f32 && pl.col_tiles == 1 && units * pl.tiles * packed_tile_bytes(s.head_dim) >= (int64_t)128 << 20;
+  pl.past_caches = !f32 && pl.col_tiles == 1 && (double)units * pl.tiles * packed_tile_bytes(s.head_dim) >= 128 << 20;
   if (pl.n_split > 1) {
     pl.part_o_bytes = align_up((size_t)units * pl.n_split * 32 * s.head_dim * sizeof(float));
     pl.part_ml_bytes = align_up((size_t)units * pl.n_split * 2 * 32 * sizeof(float));
@@ -899,9 +907,11 @@ int32_t sdllm_workspace_bytes(const sdllm_shape_t* shape, int32_t op, int32_t n_
       break;
     case SDLLM_OP_SPARSE_ATTN_PACKED:
       if (n_cached < 0) return SDLLM_ERR_INVALID_ARG;
+      if (!heads_fit(s)) return SDLLM_ERR_UNSUPPORTED;
       need = plan_packed(s, n_cached).ws_bytes();
       break;
     case SDLLM_OP_BLOCK_STEP_PACKED:
+      if (!heads_fit(s)) return SDLLM_ERR_UNSUPPORTED;
       need = packed_step_bytes(s);
       break;
     default: return SDLLM_ERR_INVALID_ARG;
@@ -1009,17 +1019,19 @@ int32_t sdllm_block_step(const sdllm_shape_t* shape, int32_t step_in_block, int3
 }
 
 int32_t sdllm_packed_cache_bytes(const sdllm_shape_t* shape, int32_t cache_rows, size_t* bytes) {
-  const int32_t st = check_shape(shape);
+  const int32_t st = check_packed_shape(shape);
   if (st != SDLLM_OK) return st;
   if (!bytes || cache_rows < 0) return SDLLM_ERR_INVALID_ARG;
-  const size_t need = (size_t)shape->batch * shape->n_kv_heads * packed_head_bytes(*shape, cache_rows);
+  const int64_t heads = (int64_t)shape->batch * shape->n_kv_heads, head = packed_head_bytes(*shape, cache_rows);
+  if (head > INT64_MAX / heads) return SDLLM_ERR_UNSUPPORTED;
+  const size_t need = (size_t)(heads * head);
   *bytes = need > 0 ? need : kAlign;   // never zero, so callers can always allocate
   return SDLLM_OK;
 }
 
 int32_t sdllm_compact_kv_packed(const sdllm_shape_t* shape, const void* k_full, const void* v_full, const int32_t* idx, void* cache,
                                 int32_t cache_rows, void* stream) {
-  int32_t st = check_shape(shape);
+  int32_t st = check_packed_shape(shape);
   if (st != SDLLM_OK) return st;
   const sdllm_shape_t& s = *shape;
   const int32_t n = counts_of(s).k_total;
@@ -1034,7 +1046,7 @@ int32_t sdllm_compact_kv_packed(const sdllm_shape_t* shape, const void* k_full, 
 }
 
 int32_t sdllm_unpack_kv(const sdllm_shape_t* shape, const void* cache, int32_t cache_rows, int32_t n_cached, void* k_out, void* v_out, void* stream) {
-  int32_t st = check_shape(shape);
+  int32_t st = check_packed_shape(shape);
   if (st != SDLLM_OK) return st;
   const sdllm_shape_t& s = *shape;
   if ((st = check_packed(cache, cache_rows, n_cached)) != SDLLM_OK) return st;
@@ -1049,7 +1061,7 @@ int32_t sdllm_unpack_kv(const sdllm_shape_t* shape, const void* cache, int32_t c
 
 int32_t sdllm_sparse_attn_packed(const sdllm_shape_t* shape, const void* q_blk, const void* cache, int32_t cache_rows, int32_t n_cached,
                                  const void* k_blk, const void* v_blk, void* out, void* ws, size_t ws_bytes, void* stream) {
-  int32_t st = check_shape(shape);
+  int32_t st = check_packed_shape(shape);
   if (st != SDLLM_OK) return st;
   const sdllm_shape_t& s = *shape;
   if ((st = check_q(s, q_blk)) != SDLLM_OK) return st;
@@ -1081,7 +1093,7 @@ int32_t sdllm_sparse_attn_packed(const sdllm_shape_t* shape, const void* q_blk, 
 int32_t sdllm_block_step_packed(const sdllm_shape_t* shape, int32_t step_in_block, int32_t delay, const void* q_blk, const void* k_in,
                                 const void* v_in, int32_t* idx, void* cache, int32_t cache_rows, void* out, void* ws, size_t ws_bytes,
                                 void* stream, int32_t* state_out) {
-  int32_t st = check_shape(shape);
+  int32_t st = check_packed_shape(shape);
   if (st != SDLLM_OK) return st;
   const sdllm_shape_t& s = *shape;
   int32_t state;
@@ -1209,7 +1221,7 @@ int32_t sdllm_launch_plan(const sdllm_shape_t* shape, int32_t call, int32_t n_ca
 }
 
 int32_t sdllm_packed_plan(const sdllm_shape_t* shape, int32_t n_cached, sdllm_packed_plan_t* plan) {
-  const int32_t st = check_shape(shape);
+  const int32_t st = check_packed_shape(shape);
   if (st != SDLLM_OK) return st;
   if (!plan || n_cached < 0) return SDLLM_ERR_INVALID_ARG;
   const PackedPlan pl = plan_packed(*shape, n_cached);
