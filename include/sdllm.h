@@ -295,7 +295,7 @@ int32_t sdllm_block_step_packed(const sdllm_shape_t* shape, int32_t step_in_bloc
 typedef struct sdllm_qk_shape {
   int32_t batch;       /* B >= 1 */
   int32_t n_q_heads;   /* >= 0 */
-  int32_t n_kv_heads;  /* >= 0, not both 0 */
+  int32_t n_kv_heads;  /* >= 0, not both 0, and no more than 2^30 together */
   int32_t head_dim;    /* 64 or 128 */
   int32_t rows;        /* n >= 0 positions */
   int32_t dtype;       /* SDLLM_BF16 | SDLLM_F32 */

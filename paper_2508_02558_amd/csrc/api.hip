@@ -1126,6 +1126,8 @@ int32_t sdllm_qk_norm_rope(const sdllm_qk_shape_t* shape, const void* q_in, cons
     return SDLLM_ERR_INVALID_ARG;
   if (!(s.eps >= 0.f) || !isfinite(s.eps)) return SDLLM_ERR_INVALID_ARG;
   if (s.head_dim != 64 && s.head_dim != 128) return SDLLM_ERR_UNSUPPORTED;
+  // a wavefront steps over heads in 32 bits, by 2^18 at most
+  if ((int64_t)s.n_q_heads + s.n_kv_heads > (int64_t)1 << 30) return SDLLM_ERR_UNSUPPORTED;
   if (s.rot_dim < 0 || s.rot_dim > s.head_dim || s.rot_dim % 2 != 0) return SDLLM_ERR_INVALID_ARG;
   if (s.rot_dim % 16 != 0) return SDLLM_ERR_UNSUPPORTED;
   if (s.rot_dim > 0 && !inv_freq) return SDLLM_ERR_INVALID_ARG;
