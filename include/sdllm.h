@@ -285,7 +285,7 @@ int32_t sdllm_block_step_packed(const sdllm_shape_t* shape, int32_t step_in_bloc
  * then the pairs (a, b) of its first rot_dim channels are turned by t = position * inv_freq[f], f = 0 .. rot_dim/2 - 1:
  *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),
  * pair f being channels (f, f + rot_dim/2) (SDLLM_PAIR_HALVES) or (2 f, 2 f + 1) (SDLLM_PAIR_ADJACENT).  fp32 throughout and one
- * rounding at the end; t is formed and reduced in 64 bits.
+ * rounding at the end; rows may be of any magnitude, also where x^2 is no number of fp32; t is formed and reduced in 64 bits.
  */
 #define SDLLM_NORM_NONE 0
 #define SDLLM_NORM_RMS 1
