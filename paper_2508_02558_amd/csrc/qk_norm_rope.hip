@@ -1,7 +1,7 @@
 // Norm of each query and key head and rotation by position in one pass: what turns a projection into the q_blk and k_in of a block
 // step.  y = x / sqrt(mean(x^2) + eps) * w per head, then each pair (a, b) of frequency f becomes (a cos t - b sin t, a sin t + b cos t), t =
-// position * inv_freq[f].  fp32 throughout, one rounding at the end; t in 64 bits, reduced to a part of a turn before it
-// is rounded, because 32 bits leave of an angle of 10^5 no more than 2^-7.
+// position * inv_freq[f].  fp32 throughout, one rounding at the end; t in 64 bits, reduced to a part of a turn, because 32 bits leave of an angle of
+// 10^5 no more than 2^-7, and what rounding that part to 32 bits leaves off goes into its sine and cosine.
 //
 // Bound by memory.  A lane holds the two 16-byte pieces of a head that are turned into each other, 4 to 16 lanes a head, and a wavefront
 // 4 to 16 heads of one position, so that an angle is computed once by one lane and handed to the others.
@@ -43,7 +43,13 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(const QkPara
     const int position = p.positions ? p.positions[b * p.pos_stride + row] : p.pos_begin + row;
     double turns = (double)position * (double)p.inv_freq[lane] * 0.15915494309189533577;
     turns -= rint(turns);
-    sincospif((float)(2.0 * turns), &sn, &cs);
+    // in half turns, as a float and what that leaves off: sine and cosine of their sum, to first order
+    const double half_turns = 2.0 * turns;
+    const float near = (float)half_turns, rest = 3.14159265f * (float)(half_turns - (double)near);
+    float s0, c0;
+    sincospif(near, &s0, &c0);
+    sn = __builtin_fmaf(c0, rest, s0);
+    cs = __builtin_fmaf(-s0, rest, c0);
   }
   float c[N], s[N];
 #pragma unroll
