@@ -50,7 +50,8 @@ class Layer:
 
 def decode_block(layer, x_full, x_steps, block_off, block_len, *, packed=True, retention=0.5, delay=1):
     """Outputs [steps, B, Hq, b, d] of a block's denoising steps.  x_full [B, L, hidden]: the layer's input of the whole sequence;
-    x_steps [steps, B, b, hidden]: that of the block, which a step changes.  Also the cache, the retained positions, and the last step's call."""
+    x_steps [steps, B, b, hidden]: that of the block, which a step changes.  Also the cache, the retained positions, and the call of the last
+    step that read the cache (None if there was none)."""
     batch, L, _ = x_full.shape
     hq, hkv, d, o, b = layer.q_heads, layer.kv_heads, layer.head_dim, block_off, block_len
     row = (hq + 2 * hkv) * d
@@ -86,7 +87,7 @@ def decode_block(layer, x_full, x_steps, block_off, block_len, *, packed=True, r
             x[:, o:o + b] = x_steps[t]
             q, k, v = layer.qkv(x, 0)
             step(t, q[:, :, o:o + b], k, v, shapes[L])
-    return out, cache, idx, (lambda: step(*last))
+    return out, cache, idx, last and (lambda: step(*last))
 
 
 def inputs(batch, seq_len, block_off, block_len, hidden, steps, seed=1):
@@ -115,6 +116,8 @@ def main():
     for name, default in (("batch", 1), ("prompt", 4096), ("gen", 256), ("block", 32), ("q-heads", 28), ("kv-heads", 4), ("hidden", 2048), ("steps", 32)):
         ap.add_argument("--" + name, type=int, default=default)
     a = ap.parse_args()
+    if a.steps < 3:
+        ap.error("--steps: the third is the first that reuses the cache")
     layer = Layer(a.hidden, a.q_heads, a.kv_heads)
     x, x_steps = inputs(a.batch, a.prompt + a.gen, a.prompt, a.block, a.hidden, a.steps)
     got = {}
@@ -123,8 +126,7 @@ def main():
         got[packed] = out.float()
         held = sum(c.numel() * c.element_size() for c in cache)
         print(f"{'4 bits' if packed else 'bf16':>7}: cache {held / 2 ** 20:8.2f} MiB, step over it {_time_us(reuse):7.2f} us")
-    t0 = 2 if a.steps > 2 else 0
-    diff = (got[True][t0:] - got[False][t0:]).norm() / got[False][t0:].norm()
+    diff = (got[True][2:] - got[False][2:]).norm() / got[False][2:].norm()
     print(f"outputs of the steps that reuse the cache: {diff:.3f} apart (relative, 2-norm)")
 
 
