@@ -702,11 +702,11 @@ PackedPlan plan_packed(const sdllm_shape_t& s, int32_t n_cached) {
   // Key splits, measured with one workgroup of up to eight wavefronts per CU (bf16, head_dim 128, 32 columns; us per call).  A tile more in a
   // workgroup is 0.1; a split is a workgroup's fixed 6 again, in parallel, a second launch (2), and partials that are written, read and folded
   // (0.1 and 0.014 for each unit of work, i.e. KV head and 32 columns; folded are the columns that there are).  The sum is least at
-  // sqrt(0.1 tiles / that): 28 units x 260 14.2 with 7, 14.8 with 9; 8 x 125 10.0 with 8, 11.3 with 4; 2 x 125 9.8 with 8, 11.2 with 4; 8 units of
-  // 8 columns x 188 tiles of 64 channels 8.7 with 12, 9.25 with 9; unsplit where that saves less than it costs: 32 x 20 8.0 against 8.8,
-  // 112 x 68 13.5 against 14.6 (96 x 94 16.4 against 15.2).  One more where that takes the wavefronts a round less: 28 x 68 10.43 with 5, 10.57 with 4,
-  // 28 x 125 11.74 with 6, 11.96 with 5, 8 of 4 columns x 47 8.3 with 7, 9.0 with 6.  None just past a multiple of eight, as the merge reads eight at
-  // a time: 8 x 125 10.2 with 8, 10.6 with 9, one of 4 columns x 625 12.0 with 23, 13.0 with 25.  fp32 takes four times as long for a tile: 4 x 38 12.2 with
+  // sqrt(0.1 tiles / that): 28 units x 260 13.9 with 7, 14.3 with 9; 8 x 125 10.0 with 8, 11.5 with 4; 2 x 125 9.6 with 8, 11.3 with 4; 8 units of
+  // 8 columns x 188 tiles of 64 channels 8.7 with 12, 9.3 with 9; unsplit where that saves less than it costs: 32 x 20 8.0 against 9.4,
+  // 112 x 68 14.3 against 14.7 (96 x 94 17.2 against 16.2).  One more where that takes the wavefronts a round less: 28 x 68 10.4 with 5, 10.5 with 4,
+  // 28 x 125 11.7 with 6, 12.0 with 5, 8 of 4 columns x 47 8.2 with 7, 9.0 with 6.  None just past a multiple of eight, as the merge reads eight at
+  // a time: 8 x 125 10.0 with 8, 10.6 with 9, one of 4 columns x 625 11.9 with 23, 12.9 with 25.  fp32 takes four times as long for a tile: 4 x 38 12.2 with
   // 10, 14.4 with 8, 22 unsplit.
   const int waves = f32 ? kPackedWavesF32 : kPackedWavesBf16;
   auto rounds_of = [&](int splits) { return ((pl.tiles + splits - 1) / splits + pl.blk_tiles + waves - 1) / waves; };
@@ -720,14 +720,14 @@ PackedPlan plan_packed(const sdllm_shape_t& s, int32_t n_cached) {
   pl.n_split = pl.tiles > 0 ? (pl.tiles + pl.tiles_per_split - 1) / pl.tiles_per_split : 1;
   // Wavefronts: the fewest that take no more rounds than the most do (32 x 20 tiles and the block's 8.2 us with seven, 8.45 with eight).  With
   // more units than CUs the LDS of four lets two workgroups share a CU, one setting up or merging while the other multiplies (512 units x 69 tiles
-  // 37.3 us, with eight wavefronts 41.1; 288 x 17 12.3, 16.8); with head_dim 64 two of eight fit.
+  // 34.5 us, with eight wavefronts 39.0; 288 x 17 12.5, 16.6); with head_dim 64 two of eight fit.
   int most_waves = waves;
   if (units * pl.n_split > kNumCUs && s.head_dim == 128) most_waves = 4;
   const int rounds = (pl.tiles_per_split + pl.blk_tiles + most_waves - 1) / most_waves;
   pl.waves = (pl.tiles_per_split + pl.blk_tiles + rounds - 1) / rounds;
   // Past the caches where every tile is read once and two such calls would not fit the memory-side cache (256 MB) together: 512 units x 69
-  // tiles, 150 MB, 37.6 -> 34.5 us, 256 x 69, 75 MB, 22.0 -> 20.5 us with 900 MB of other caches read in between, but 18.6 -> 20.5 with 150 MB.
-  // Tiles that several blocks of columns read come from L2: 224 x 73 15.9 -> 16.7.
+  // tiles, 150 MB, 37.3 -> 34.5 us, 256 x 69, 75 MB, 22.0 -> 20.5 us with 900 MB of other caches read in between, but 18.9 -> 19.8 with 150 MB.
+  // Tiles that several blocks of columns read come from L2: 224 x 73 15.8 -> 15.9.
   pl.past_caches = !f32 && pl.col_tiles == 1 && (double)units * pl.tiles * packed_tile_bytes(s.head_dim) >= 128 << 20;
   if (pl.n_split > 1) {
     pl.part_o_bytes = align_up((size_t)units * pl.n_split * 32 * s.head_dim * sizeof(float));

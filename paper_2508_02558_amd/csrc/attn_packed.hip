@@ -11,13 +11,13 @@
 // folds.
 //
 // What bounds it.  Calls on few heads: latency; a workgroup is 5 us without its tiles, 2.3 of them the launch, 1.4 until the queries are
-// there, 1.5 to 2 for the merge (16 KB of LDS a wavefront, in and out).  Full grids: a tile is 580 cycles of vector and 512 of matrix instructions
-// to a SIMD (measured rates: 4.5 cycles a conversion, fma or add, 8 an exponential, 32 and 64 the matrix instructions) and takes 1150 with two
-// wavefronts there; fetches held up by memory are 2 of 15 us with 224 workgroups x 73 tiles and 6 of 21 with 256 x 69 from HBM (3.9 TB/s; 18 us from
-// the memory-side cache).
-// Measured and not kept: sums and maxima between the products of the values, where the matrix unit has room for them (within 1%); a higher priority
-// for wavefronts that are there (224 x 73 -1.5%, 256 x 69 from HBM +4%); LDS for each wavefront to park its results in without waiting
-// (+1 to +4%: the code is longer); four wavefronts instead of eight (224 x 73 17.1 us in place of 14.6).
+// there, 1.5 to 2 for the merge (16 KB of LDS a wavefront, in and out).  Full grids: a tile is 750 cycles of vector and 512 of matrix instructions
+// to a SIMD (measured rates: 4.5 cycles a conversion, fma or add, 8 an exponential, 32 a matrix instruction) and takes 1265 of it, their sum, although
+// two wavefronts are there: 224 workgroups x 73 tiles keep the matrix unit busy for 31 % of 15.7 us.  256 x 69 from HBM take 21.4 to 22 us
+// (3.9 TB/s), 18.2 to 18.9 from the memory-side cache.
+// Measured, when calls of four tiles a wavefront and more were 2 to 3 % faster, and not kept: sums and maxima between the products of the values, where the
+// matrix unit has room for them (within 1%); a higher priority for wavefronts that are there (224 x 73 -1.5%, 256 x 69 from HBM +4%); LDS for each
+// wavefront to park its results in without waiting (+1 to +4%: the code is longer).  Four wavefronts instead of eight: 224 x 73 17.7 us in place of 15.8.
 #include "attn_merge.h"
 #include "attn_tile_math.h"
 #include "packed_tile.h"
@@ -419,7 +419,7 @@ __global__ __launch_bounds__(Parts<T>::kWaves * kWave) void attn_packed_kernel(c
     float m_loc;                                         // of the tile whose logits are there
     // One tile: its softmax and its product with the values, and the next tile's logits.  While a matrix instruction waits, for the one before
     // it or for the unit, nothing of any wavefront is issued to the SIMD's vector units; so each is followed by as many vector instructions as
-    // it takes, in this order (the barriers keep the compiler from gathering them).
+    // it takes, in this order (the barriers keep the compiler from gathering them).  Little overlaps all the same: a tile takes the sum of both times.
     auto step = [&](auto parity_tag, f32x16& s, f32x16& s_next) {
       constexpr int kParity = decltype(parity_tag)::value;
       ring.arrived();
