@@ -78,6 +78,9 @@ extern "C" {
 #define SDLLM_OP_BLOCK_STEP 3
 #define SDLLM_OP_SPARSE_ATTN_PACKED 4
 #define SDLLM_OP_BLOCK_STEP_PACKED 5
+/* for sdllm_paged_workspace_bytes */
+#define SDLLM_OP_TREE_ATTN_PAGED 6
+#define SDLLM_OP_WINDOW_ATTN_PAGED 7
 
 typedef struct sdllm_shape {
   int32_t batch;       /* B >= 1 */
@@ -320,6 +323,85 @@ typedef struct sdllm_qk_shape {
  */
 int32_t sdllm_qk_norm_rope(const sdllm_qk_shape_t* shape, const void* q_in, const void* k_in, const void* q_weight, const void* k_weight,
                            const float* inv_freq, const int32_t* positions, void* q_out, void* k_out, void* stream);
+
+/*
+ * ---- Paged cache: sequences of unlike lengths
+ *
+ * Keys and values of a batch of sequences in pages of page_rows rows, handed out by the caller from one pool: row j of sequence b is row
+ * j % page_rows of page table[b][j / page_rows].  sdllm_append_paged puts new rows there, normalised and turned on the way;
+ * sdllm_tree_attn_paged attends from a block of rows, or a tree of drafted tokens, that are in no page yet; sdllm_window_attn_paged from rows that
+ * are.  A step of a decoder calls them with the same `lengths`, `row_counts` and `table`:
+ *   k_pages/v_pages [n_pages, Hkv, page_rows, d], page_stride between pages, heads and rows;
+ *   table           int32 [B, table_pages], table_stride elements between sequences: pages of the pool.  Several sequences may name the same page
+ *                   to share its rows.  Entries that no row in use falls in are not looked at.  An entry outside the pool is read as the nearest page of it, and not written to;
+ *   lengths         int32 [B]: rows that sequence b has before the new ones, held to [0, table_pages * page_rows] (nothing if the pool is empty);
+ *   row_counts      int32 [B]: new rows of sequence b, held to [0, rows]; NULL: `rows` each.  Rows from there on are not read, and outputs are left as they were there.
+ * Integers are device memory, so that a captured graph takes those of its replay.  Pages are never allocated, moved or cleared.
+ *
+ * Both attentions run with fp32 sums; with bf16 tensors the softmax numerators are rounded to bf16 for the product with the values.  A row that sees no
+ * key is zero.  What a row does not see takes no part in its result, whatever it holds (infinities and NaN included).
+ */
+typedef struct sdllm_paged_shape {
+  int32_t batch;        /* B >= 1 sequences */
+  int32_t n_q_heads;    /* Hq, multiple of n_kv_heads */
+  int32_t n_kv_heads;   /* Hkv >= 1 */
+  int32_t head_dim;     /* d in {64, 128} */
+  int32_t rows;         /* n >= 0 new rows of a sequence, or the most that row_counts names; <= 64 for sdllm_tree_attn_paged, <= 2^29 */
+  int32_t dtype;        /* SDLLM_BF16 | SDLLM_F32 */
+  int32_t n_pages;      /* pages of the pool, >= 0 */
+  int32_t page_rows;    /* 16, 32, 64, 128 or 256 */
+  int32_t table_pages;  /* >= 0 entries of a sequence's row of the table; table_pages * page_rows <= 2^29 */
+  int32_t window_left;  /* sdllm_window_attn_paged: keys before its own that a row sees; negative: all */
+  int32_t window_right; /* ... and behind it; negative: all */
+  int32_t sinks;        /* ... and first keys of the sequence that it sees besides, >= 0 */
+  float softmax_scale;  /* 0 means 1/sqrt(head_dim) */
+  int32_t reserved;     /* must be 0 */
+  int64_t table_stride; /* elements between the sequences' rows of the table */
+  int64_t mask_stride;  /* elements between the sequences' masks; 0: the same for all */
+  /* element strides; the last axis (head_dim) is contiguous */
+  int64_t q_stride[3];    /* {batch, head, row} of queries       [B, Hq,  n, d] */
+  int64_t blk_stride[3];  /* of k_blk and v_blk                  [B, Hkv, n, d] */
+  int64_t out_stride[3];  /* of the output                       [B, Hq,  n, d] */
+  int64_t page_stride[3]; /* {page, head, row} of the pages      [n_pages, Hkv, page_rows, d] */
+} sdllm_paged_shape_t;
+
+/* Bytes of device workspace that SDLLM_OP_TREE_ATTN_PAGED or SDLLM_OP_WINDOW_ATTN_PAGED needs for this shape, whatever the lengths; the attentions take no less.
+ * Host call. */
+int32_t sdllm_paged_workspace_bytes(const sdllm_paged_shape_t* shape, int32_t op, size_t* bytes);
+
+/*
+ * sdllm_qk_norm_rope of queries and keys with the keys, and the values as they are, going to the pages: row i of sequence b to its cache row
+ * lengths[b] + i.  Rows that the table has no room or no page for are not written.  q_in/q_out/weights/inv_freq as there (qk->k_out_stride is not read; n_q_heads may be 0);
+ * v_in [B, Hkv, n, d] has the strides of k_in.  q_out may be q_in, with the same strides; nothing else may overlap.
+ *   positions int32 [B, n] of the rows of q_in and k_in, n contiguous (qk->pos_stride between sequences), or NULL: lengths[b] + qk->pos_begin + i;
+ *   pick      int32 [B, n], n contiguous, or NULL.  Row i that is appended is then row pick[b][i] of k_in and v_in (held to [0, n)), with
+ *             that row's position if there are positions: what is left of a tree of drafted tokens.  Only with n_q_heads of 0.
+ * Of `shape` the cache's fields are read; batch, n_kv_heads, head_dim, rows and dtype have to be those of qk.
+ * Two rows of one call must not go to the same place.
+ */
+int32_t sdllm_append_paged(const sdllm_qk_shape_t* qk, const sdllm_paged_shape_t* shape, const void* q_in, const void* k_in, const void* v_in,
+                           const void* q_weight, const void* k_weight, const float* inv_freq, const int32_t* positions, const int32_t* pick,
+                           const int32_t* lengths, const int32_t* row_counts, const int32_t* table, void* q_out, void* k_pages, void* v_pages,
+                           void* stream);
+
+/*
+ * out[b,h,i] = sum_j softmax_j(scale <q[b,h,i], k_j>) v_j over the lengths[b] cache rows of sequence b and those of its own new rows j that row i sees:
+ * bit j of mask[b][i].  k_blk/v_blk [B, Hkv, n, d] (blk_stride) are the new rows' keys and values.  mask uint64 [B, n], n contiguous
+ * (mask_stride between sequences); NULL: every row sees all new rows of its sequence, as a block of the paper does.  rows <= 64.
+ * ws of sdllm_paged_workspace_bytes(SDLLM_OP_TREE_ATTN_PAGED), aligned to 256 bytes.
+ */
+int32_t sdllm_tree_attn_paged(const sdllm_paged_shape_t* shape, const void* q, const void* k_pages, const void* v_pages, const int32_t* table,
+                              const int32_t* lengths, const int32_t* row_counts, const void* k_blk, const void* v_blk, const uint64_t* mask,
+                              void* out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The same over the cache alone, for rows that have been appended: row i of sequence b is at place p = lengths[b] + i of its
+ * lengths[b] + row_counts[b] rows and sees row j of them if j <= p + window_right and (j >= p - window_left or j < sinks), a negative
+ * window_left or window_right being no limit.  {-1, 0, 0} is causal attention, {-1, -1, 0} full attention.  Pages of which
+ * no row is seen are not read.  ws of sdllm_paged_workspace_bytes(SDLLM_OP_WINDOW_ATTN_PAGED), aligned to 256 bytes.
+ */
+int32_t sdllm_window_attn_paged(const sdllm_paged_shape_t* shape, const void* q, const void* k_pages, const void* v_pages, const int32_t* table,
+                                const int32_t* lengths, const int32_t* row_counts, void* out, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -27,6 +27,7 @@ SDLLM_EVICT_BIDIRECTIONAL, SDLLM_EVICT_PREFIX_ONLY = 0, 1
 SDLLM_STATE_FULL, SDLLM_STATE_UPDATE, SDLLM_STATE_REUSE = 0, 1, 2
 SDLLM_OP_SCORE_SELECT, SDLLM_OP_COMPACT_KV, SDLLM_OP_SPARSE_ATTN, SDLLM_OP_BLOCK_STEP = 0, 1, 2, 3
 SDLLM_OP_SPARSE_ATTN_PACKED, SDLLM_OP_BLOCK_STEP_PACKED = 4, 5
+SDLLM_OP_TREE_ATTN_PAGED, SDLLM_OP_WINDOW_ATTN_PAGED = 6, 7
 SDLLM_NORM_NONE, SDLLM_NORM_RMS = 0, 1
 SDLLM_PAIR_HALVES, SDLLM_PAIR_ADJACENT = 0, 1
 
@@ -34,7 +35,8 @@ EXPORTED = ("sdllm_error_string", "sdllm_version", "sdllm_retained_count", "sdll
             "sdllm_cache_state", "sdllm_score_select", "sdllm_compact_kv", "sdllm_sparse_attn",
             "sdllm_sparse_attn_noalloc", "sdllm_block_step", "sdllm_dense_attn", "sdllm_packed_cache_bytes",
             "sdllm_compact_kv_packed", "sdllm_unpack_kv", "sdllm_sparse_attn_packed", "sdllm_block_step_packed",
-            "sdllm_qk_norm_rope", "sdllm_stream_read_probe",
+            "sdllm_qk_norm_rope", "sdllm_paged_workspace_bytes", "sdllm_append_paged", "sdllm_tree_attn_paged", "sdllm_window_attn_paged",
+            "sdllm_stream_read_probe",
             "sdllm_launch_plan", "sdllm_packed_plan", "sdllm_burst_splits", "sdllm_dense_tail_groups",
             "sdllm_column_kernel")
 
@@ -64,6 +66,16 @@ class sdllm_qk_shape_t(ctypes.Structure):
         ("norm", ctypes.c_int32), ("eps", ctypes.c_float), ("pos_begin", ctypes.c_int32), ("reserved", ctypes.c_int32),
         ("pos_stride", ctypes.c_int64), ("q_in_stride", ctypes.c_int64 * 3), ("k_in_stride", ctypes.c_int64 * 3),
         ("q_out_stride", ctypes.c_int64 * 3), ("k_out_stride", ctypes.c_int64 * 3),
+    ]
+
+
+class sdllm_paged_shape_t(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("rows", ctypes.c_int32), ("dtype", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+        ("table_pages", ctypes.c_int32), ("window_left", ctypes.c_int32), ("window_right", ctypes.c_int32), ("sinks", ctypes.c_int32),
+        ("softmax_scale", ctypes.c_float), ("reserved", ctypes.c_int32), ("table_stride", ctypes.c_int64), ("mask_stride", ctypes.c_int64),
+        ("q_stride", ctypes.c_int64 * 3), ("blk_stride", ctypes.c_int64 * 3), ("out_stride", ctypes.c_int64 * 3), ("page_stride", ctypes.c_int64 * 3),
     ]
 
 
@@ -131,6 +143,15 @@ def load() -> ctypes.CDLL:
     lib.sdllm_block_step_packed.argtypes = [shp, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, sz, vp, i32p]
     lib.sdllm_qk_norm_rope.restype = i32
     lib.sdllm_qk_norm_rope.argtypes = [ctypes.POINTER(sdllm_qk_shape_t), vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    paged = ctypes.POINTER(sdllm_paged_shape_t)
+    lib.sdllm_paged_workspace_bytes.restype = i32
+    lib.sdllm_paged_workspace_bytes.argtypes = [paged, i32, ctypes.POINTER(sz)]
+    lib.sdllm_append_paged.restype = i32
+    lib.sdllm_append_paged.argtypes = [ctypes.POINTER(sdllm_qk_shape_t), paged] + [vp] * 15
+    lib.sdllm_tree_attn_paged.restype = i32
+    lib.sdllm_tree_attn_paged.argtypes = [paged] + [vp] * 11 + [sz, vp]
+    lib.sdllm_window_attn_paged.restype = i32
+    lib.sdllm_window_attn_paged.argtypes = [paged] + [vp] * 8 + [sz, vp]
     lib.sdllm_stream_read_probe.restype = i32
     lib.sdllm_stream_read_probe.argtypes = [vp, sz, vp, vp]
     lib.sdllm_launch_plan.restype = i32
@@ -254,6 +275,25 @@ def make_qk_shape(*, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int,
     for name, val, heads in (("q_in_stride", q_in_stride, n_q_heads), ("k_in_stride", k_in_stride, n_kv_heads),
                              ("q_out_stride", q_out_stride, n_q_heads), ("k_out_stride", k_out_stride, n_kv_heads)):
         v = tuple(val) if val is not None else (heads * rows * head_dim, rows * head_dim, head_dim)
+        setattr(s, name, (ctypes.c_int64 * 3)(*v))
+    return s
+
+
+def make_paged_shape(*, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, rows: int, dtype: int, n_pages: int, page_rows: int,
+                     table_pages: int, window_left: int = -1, window_right: int = 0, sinks: int = 0, softmax_scale: float = 0.0,
+                     table_stride: Optional[int] = None, mask_stride: Optional[int] = None, q_stride: Optional[Sequence[int]] = None,
+                     blk_stride: Optional[Sequence[int]] = None, out_stride: Optional[Sequence[int]] = None,
+                     page_stride: Optional[Sequence[int]] = None) -> sdllm_paged_shape_t:
+    """Fill an sdllm_paged_shape_t; strides left out default to dense tensors, the window to causal attention."""
+    s = sdllm_paged_shape_t()
+    s.batch, s.n_q_heads, s.n_kv_heads, s.head_dim, s.rows, s.dtype = batch, n_q_heads, n_kv_heads, head_dim, rows, dtype
+    s.n_pages, s.page_rows, s.table_pages = n_pages, page_rows, table_pages
+    s.window_left, s.window_right, s.sinks, s.softmax_scale, s.reserved = window_left, window_right, sinks, softmax_scale, 0
+    s.table_stride = table_pages if table_stride is None else table_stride
+    s.mask_stride = rows if mask_stride is None else mask_stride
+    for name, val, heads, n in (("q_stride", q_stride, n_q_heads, rows), ("blk_stride", blk_stride, n_kv_heads, rows),
+                                ("out_stride", out_stride, n_q_heads, rows), ("page_stride", page_stride, n_kv_heads, page_rows)):
+        v = tuple(val) if val is not None else (heads * n * head_dim, n * head_dim, head_dim)
         setattr(s, name, (ctypes.c_int64 * 3)(*v))
     return s
 
@@ -393,6 +433,44 @@ def sdllm_qk_norm_rope(shape, q_in, k_in, q_weight, k_weight, inv_freq, position
         return
     _check(load().sdllm_qk_norm_rope(ctypes.byref(shape), _ptr(q_in), _ptr(k_in), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
                                      _ptr(positions), _ptr(q_out), _ptr(k_out), _stream(stream)), "sdllm_qk_norm_rope")
+
+
+def sdllm_paged_workspace_bytes(shape: sdllm_paged_shape_t, op: int) -> int:
+    out = ctypes.c_size_t()
+    _check(load().sdllm_paged_workspace_bytes(ctypes.byref(shape), op, ctypes.byref(out)), "sdllm_paged_workspace_bytes")
+    return out.value
+
+
+def sdllm_append_paged(qk, shape, q_in, k_in, v_in, q_weight, k_weight, inv_freq, positions, pick, lengths, row_counts, table, q_out, k_pages,
+                       v_pages, stream=None) -> None:
+    if _pycall is not None and isinstance(qk, sdllm_qk_shape_t) and isinstance(shape, sdllm_paged_shape_t):
+        _check(_pycall.append_paged(_address("sdllm_append_paged"), ctypes.addressof(qk), ctypes.addressof(shape), q_in, k_in, v_in, q_weight, k_weight,
+                                    inv_freq, positions, pick, lengths, row_counts, table, q_out, k_pages, v_pages, _stream(stream) or 0),
+               "sdllm_append_paged")
+        return
+    _check(load().sdllm_append_paged(ctypes.byref(qk), ctypes.byref(shape), _ptr(q_in), _ptr(k_in), _ptr(v_in), _ptr(q_weight), _ptr(k_weight),
+                                     _ptr(inv_freq), _ptr(positions), _ptr(pick), _ptr(lengths), _ptr(row_counts), _ptr(table), _ptr(q_out),
+                                     _ptr(k_pages), _ptr(v_pages), _stream(stream)), "sdllm_append_paged")
+
+
+def sdllm_tree_attn_paged(shape, q, k_pages, v_pages, table, lengths, row_counts, k_blk, v_blk, mask, out, ws, stream=None) -> None:
+    if _pycall is not None and isinstance(shape, sdllm_paged_shape_t):
+        _check(_pycall.tree_attn_paged(_address("sdllm_tree_attn_paged"), ctypes.addressof(shape), q, k_pages, v_pages, table, lengths, row_counts,
+                                       k_blk, v_blk, mask, out, ws, _stream(stream) or 0), "sdllm_tree_attn_paged")
+        return
+    _check(load().sdllm_tree_attn_paged(ctypes.byref(shape), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table), _ptr(lengths), _ptr(row_counts),
+                                        _ptr(k_blk), _ptr(v_blk), _ptr(mask), _ptr(out), _ptr(ws),
+                                        ws.numel() * ws.element_size() if ws is not None else 0, _stream(stream)), "sdllm_tree_attn_paged")
+
+
+def sdllm_window_attn_paged(shape, q, k_pages, v_pages, table, lengths, row_counts, out, ws, stream=None) -> None:
+    if _pycall is not None and isinstance(shape, sdllm_paged_shape_t):
+        _check(_pycall.window_attn_paged(_address("sdllm_window_attn_paged"), ctypes.addressof(shape), q, k_pages, v_pages, table, lengths, row_counts,
+                                         out, ws, _stream(stream) or 0), "sdllm_window_attn_paged")
+        return
+    _check(load().sdllm_window_attn_paged(ctypes.byref(shape), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table), _ptr(lengths), _ptr(row_counts),
+                                          _ptr(out), _ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0, _stream(stream)),
+           "sdllm_window_attn_paged")
 
 
 def sdllm_stream_read_probe(src, sink=None, stream=None) -> None:

@@ -6,18 +6,13 @@
 
 #include <algorithm>
 
-#include "sdllm.h"
+#include "api_checks.h"
 #include "sdllm_bench.h"
 #include "sdllm_internal.h"
 
 using namespace sdllm;
 
 namespace {
-
-constexpr size_t kAlign = 256;
-inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-inline int elem_size(int dtype) { return dtype == SDLLM_BF16 ? 2 : 4; }
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int32_t quota(int32_t n, double r, int32_t rounding) {
   const double x = r * (double)n;
@@ -49,12 +44,6 @@ Counts counts_of(const sdllm_shape_t& s) {
   return c;
 }
 
-bool strides_ok(const int64_t* st, int esize) {
-  for (int i = 0; i < 3; ++i)
-    if (st[i] < 0 || (st[i] * esize) % 16 != 0) return false;
-  return true;
-}
-
 int32_t check_shape(const sdllm_shape_t* s) {
   if (!s) return SDLLM_ERR_INVALID_ARG;
   if (s->batch < 1 || s->n_kv_heads < 1 || s->n_q_heads < 1 || s->n_q_heads % s->n_kv_heads != 0)
@@ -81,13 +70,9 @@ int32_t check_shape(const sdllm_shape_t* s) {
   return SDLLM_OK;
 }
 
-bool row_stride_ok(const int64_t* st, int d) { return st[2] >= d; }
-
 float scale_of(const sdllm_shape_t& s) {
   return s.softmax_scale > 0.f ? s.softmax_scale : 1.0f / sqrtf((float)s.head_dim);
 }
-
-constexpr float kLog2e = 1.4426950408889634f;
 
 // ---------------------------------------------------------------- attention planning
 struct AttnPlan {
@@ -855,6 +840,24 @@ hipError_t static_scratch(void** out) {
 }  // namespace
 
 // ================================================================ exported functions
+int32_t sdllm::check_qk_shape(const sdllm_qk_shape_t* shape) {
+  if (!shape) return SDLLM_ERR_INVALID_ARG;
+  const sdllm_qk_shape_t& s = *shape;
+  if (s.batch < 1 || s.rows < 0 || s.n_q_heads < 0 || s.n_kv_heads < 0 || (int64_t)s.n_q_heads + s.n_kv_heads < 1 ||
+      (int64_t)s.n_q_heads + s.n_kv_heads > INT32_MAX)
+    return SDLLM_ERR_INVALID_ARG;
+  if ((s.dtype != SDLLM_BF16 && s.dtype != SDLLM_F32) || (s.norm != SDLLM_NORM_NONE && s.norm != SDLLM_NORM_RMS) ||
+      (s.pairing != SDLLM_PAIR_HALVES && s.pairing != SDLLM_PAIR_ADJACENT) || s.reserved != 0)
+    return SDLLM_ERR_INVALID_ARG;
+  if (!(s.eps >= 0.f) || !isfinite(s.eps)) return SDLLM_ERR_INVALID_ARG;
+  if (s.head_dim != 64 && s.head_dim != 128) return SDLLM_ERR_UNSUPPORTED;
+  // a wavefront steps over heads in 32 bits, by 2^18 at most
+  if ((int64_t)s.n_q_heads + s.n_kv_heads > (int64_t)1 << 30) return SDLLM_ERR_UNSUPPORTED;
+  if (s.rot_dim < 0 || s.rot_dim > s.head_dim || s.rot_dim % 2 != 0) return SDLLM_ERR_INVALID_ARG;
+  if (s.rot_dim % 16 != 0) return SDLLM_ERR_UNSUPPORTED;
+  return SDLLM_OK;
+}
+
 extern "C" {
 
 const char* sdllm_error_string(int32_t status) {
@@ -1116,20 +1119,9 @@ int32_t sdllm_block_step_packed(const sdllm_shape_t* shape, int32_t step_in_bloc
 
 int32_t sdllm_qk_norm_rope(const sdllm_qk_shape_t* shape, const void* q_in, const void* k_in, const void* q_weight, const void* k_weight,
                            const float* inv_freq, const int32_t* positions, void* q_out, void* k_out, void* stream) {
-  if (!shape) return SDLLM_ERR_INVALID_ARG;
+  const int32_t st = check_qk_shape(shape);
+  if (st != SDLLM_OK) return st;
   const sdllm_qk_shape_t& s = *shape;
-  if (s.batch < 1 || s.rows < 0 || s.n_q_heads < 0 || s.n_kv_heads < 0 || (int64_t)s.n_q_heads + s.n_kv_heads < 1 ||
-      (int64_t)s.n_q_heads + s.n_kv_heads > INT32_MAX)
-    return SDLLM_ERR_INVALID_ARG;
-  if ((s.dtype != SDLLM_BF16 && s.dtype != SDLLM_F32) || (s.norm != SDLLM_NORM_NONE && s.norm != SDLLM_NORM_RMS) ||
-      (s.pairing != SDLLM_PAIR_HALVES && s.pairing != SDLLM_PAIR_ADJACENT) || s.reserved != 0)
-    return SDLLM_ERR_INVALID_ARG;
-  if (!(s.eps >= 0.f) || !isfinite(s.eps)) return SDLLM_ERR_INVALID_ARG;
-  if (s.head_dim != 64 && s.head_dim != 128) return SDLLM_ERR_UNSUPPORTED;
-  // a wavefront steps over heads in 32 bits, by 2^18 at most
-  if ((int64_t)s.n_q_heads + s.n_kv_heads > (int64_t)1 << 30) return SDLLM_ERR_UNSUPPORTED;
-  if (s.rot_dim < 0 || s.rot_dim > s.head_dim || s.rot_dim % 2 != 0) return SDLLM_ERR_INVALID_ARG;
-  if (s.rot_dim % 16 != 0) return SDLLM_ERR_UNSUPPORTED;
   if (s.rot_dim > 0 && !inv_freq) return SDLLM_ERR_INVALID_ARG;
   if (s.pos_stride < 0 || (!positions && (int64_t)s.pos_begin + s.rows > (int64_t)INT32_MAX + 1)) return SDLLM_ERR_INVALID_ARG;
   const int es = elem_size(s.dtype);

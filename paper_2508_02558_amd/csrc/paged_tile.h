@@ -1,0 +1,246 @@
+// What the kernels of the paged cache's attention share: which queries and keys a workgroup takes, and what a query row sees of a tile.
+//
+// The query rows of a KV head are columns: column c is query head c % G of the group and row c / G of the sequence, so that neighbours see nearly the same
+// keys.  A workgroup takes a block of columns (an item) and all 32-key tiles that any of them sees, or a split of those tiles.  Lengths are
+// known on the device only, so every wavefront works out the cut by itself: with W workgroups, n items and N tiles of all items together, a share is
+// c = max(least, ceil(N / (W - n))) tiles and an item with T tiles has ceil(T / c) splits; their sum is below N / c + n <= W.  Two
+// rounds of integer sums over the sequences, 64 of them at a time; nothing is kept between calls.
+#pragma once
+
+#include "mfma_tile.h"
+
+namespace sdllm {
+
+struct PagedItem {
+  int b, g, blk;            // sequence, KV head, block of columns
+  int split, n_split, slot; // slot: place of the split's partials
+  int length, count, end;   // rows before the new ones, new ones, rows that can be seen
+  int cols;                 // columns of the KV head
+  int sink_end;             // first keys that any row of the block sees as such: [0, sink_end)
+  int first, last;          // keys of the window of any row: [first, last]
+  int least_last, most_first;   // keys [most_first, least_last] are in the window of every row
+  int lead_tiles;           // tiles before the window's: of first keys, or (kSeeTree) of the cache
+  int first_tile, tiles;    // first tile of the window; tiles in all
+};
+
+__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+template <int SEES>
+__device__ __forceinline__ int last_seen(const PagedAttnParams& p, int end, int place) {
+  return p.right < 0 ? end - 1 : min(end - 1, place + p.right);
+}
+__device__ __forceinline__ int first_seen(const PagedAttnParams& p, int place) { return p.left < 0 ? 0 : max(0, place - p.left); }
+
+// Blocks of columns of a KV head
+__device__ __forceinline__ int blocks_of(const PagedAttnParams& p, int count) { return ceil_div(count * p.group, p.block_cols); }
+
+// No block of the sequence has more tiles than this
+template <int SEES>
+__device__ __forceinline__ int most_tiles(const PagedAttnParams& p, int length, int count) {
+  if (SEES == kSeeTree) return ceil_div(length, kTileKeys) + ceil_div(count, kTileKeys);
+  const int all = ceil_div(min(length + count, p.cache.capacity), kTileKeys);
+  if (p.left < 0 || p.right < 0) return all;
+  const int rows = min(count, p.block_cols / p.group + 2);   // of a block
+  return min(all, (p.left + p.right + rows) / kTileKeys + 2 + ceil_div(min(p.sinks, p.cache.capacity), kTileKeys));
+}
+
+// Rows and tiles of an item whose sequence, head and block are known
+template <int SEES>
+__device__ __forceinline__ void locate_item(const PagedAttnParams& p, PagedItem& w) {
+  w.cols = w.count * p.group;
+  w.end = SEES == kSeeTree ? w.length : min(w.length + w.count, p.cache.capacity);
+  if (SEES == kSeeTree) {
+    w.lead_tiles = ceil_div(w.length, kTileKeys);
+    w.tiles = w.lead_tiles + ceil_div(w.count, kTileKeys);
+    return;
+  }
+  const int c0 = w.blk * p.block_cols, c1 = min(c0 + p.block_cols, w.cols) - 1;
+  const int p0 = w.length + p.by_group.quotient(c0), p1 = w.length + p.by_group.quotient(c1);
+  w.first = first_seen(p, p0);
+  w.most_first = first_seen(p, p1);
+  w.least_last = last_seen<SEES>(p, w.end, p0);
+  w.last = last_seen<SEES>(p, w.end, p1);
+  w.sink_end = min(p.sinks, w.last + 1);
+  w.first_tile = w.first / kTileKeys;
+  w.lead_tiles = ceil_div(w.sink_end, kTileKeys);
+  int window = 0;
+  if (w.first <= w.last) {
+    w.lead_tiles = min(w.lead_tiles, w.first_tile);
+    window = w.last / kTileKeys - w.first_tile + 1;
+  }
+  w.tiles = w.lead_tiles + window;
+}
+
+// The item and split of this workgroup, the same for all of its threads; false: none
+template <int SEES>
+__device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, PagedItem& w) {
+  int t_most;
+  if (!p.part_o) {
+    // Items as workgroups, the last block of a head first: with all past keys to see it has the most tiles
+    const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
+    const int head = p.by_blocks.quotient(id);
+    w.blk = p.max_blocks - 1 - (id - head * p.max_blocks);
+    w.b = p.by_hkv.quotient(head);
+    w.g = head - w.b * p.hkv;
+    w.count = p.cache.count(w.b);
+    if (w.blk * p.block_cols >= w.count * p.group) return false;
+    w.length = p.cache.length(w.b);
+    w.split = 0;
+    w.n_split = 1;
+    w.slot = 0;
+    locate_item<SEES>(p, w);
+    return true;
+  }
+  struct Seq { int blocks, tiles; };
+  auto sequence = [&](int b) {
+    if (b >= p.batch) return Seq{0, 0};
+    const int count = p.cache.count(b);
+    return Seq{blocks_of(p, count), most_tiles<SEES>(p, p.cache.length(b), count)};
+  };
+  auto sum = [](auto x) {
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) x += __shfl_xor(x, o);
+    return x;
+  };
+  const Seq mine = sequence(lane);   // the first 64 sequences are looked at once
+  auto sequence_at = [&](int b0) { return b0 == 0 ? mine : sequence(b0 + lane); };
+  int items = 0;
+  double tiles = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += kWave) {
+    const Seq s = sequence_at(b0);
+    items += p.hkv * s.blocks;
+    tiles += (double)(p.hkv * s.blocks) * s.tiles;
+  }
+  items = sum(items);
+  tiles = sum(tiles);
+  // the host launches more workgroups than there can be items
+  const int share = max(p.least_tiles, (int)ceil(tiles / max(1, p.workgroups - items)));
+  int used = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += kWave) {
+    const Seq s = sequence_at(b0);
+    used += p.hkv * s.blocks * max(1, ceil_div(s.tiles, share));
+  }
+  used = sum(used);
+  if ((int)blockIdx.x >= used) return false;
+  const int id = xcd_contiguous_id(blockIdx.x, used);
+  int before = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += kWave) {
+    const Seq s = sequence_at(b0);
+    const int splits = max(1, ceil_div(s.tiles, share)), here = p.hkv * s.blocks * splits;
+    int upto = here;   // of the sequences up to this lane's
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    const uint64_t past = __ballot(id < before + upto);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      const int blocks = __builtin_amdgcn_readlane(s.blocks, l);
+      before += __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(here, l);
+      w.n_split = __builtin_amdgcn_readlane(splits, l);
+      w.b = b0 + l;
+      // those of a head and split are neighbours: they read the same keys
+      const int r = id - before, unit = r / blocks;
+      w.blk = r - unit * blocks;
+      w.g = unit / w.n_split;
+      w.split = unit - w.g * w.n_split;
+      w.slot = before + (w.g * blocks + w.blk) * w.n_split + w.split;
+      w.count = p.cache.count(w.b);
+      w.length = p.cache.length(w.b);
+      locate_item<SEES>(p, w);
+      if (w.split == 0 && threadIdx.x == 0) {
+        int32_t* at = p.item_at + 2 * ((int64_t)(w.b * p.hkv + w.g) * p.max_blocks + w.blk);
+        at[0] = w.slot;
+        at[1] = w.n_split;
+      }
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(upto, kWave - 1);
+  }
+  return false;
+}
+
+// One 32-key tile of an item.  Rows [lo, hi) of it are seen by some row of the block; the others may be anything, in pages of anybody.
+struct PagedTile {
+  bool own;      // kSeeTree: of the new rows
+  int at;        // first key
+  int lo, hi;
+  bool full;     // every row of the block sees all 32
+};
+
+template <int SEES>
+__device__ __forceinline__ PagedTile tile_of(const PagedAttnParams& p, const PagedItem& w, int t) {
+  PagedTile x;
+  if (SEES == kSeeTree) {
+    x.own = t >= w.lead_tiles;
+    x.at = (x.own ? t - w.lead_tiles : t) * kTileKeys;
+    x.lo = 0;
+    x.hi = min(kTileKeys, (x.own ? w.count : w.length) - x.at);
+    x.full = x.hi == kTileKeys && !(x.own && p.mask);
+    return x;
+  }
+  const bool lead = t < w.lead_tiles;
+  x.own = false;
+  x.at = (lead ? t : t - w.lead_tiles + w.first_tile) * kTileKeys;
+  x.lo = lead || p.sinks > x.at ? 0 : max(0, w.first - x.at);
+  x.hi = min(kTileKeys, (lead ? w.sink_end : w.last + 1) - x.at);
+  x.full = (x.at >= w.most_first || x.at + kTileKeys <= p.sinks) && x.at + kTileKeys - 1 <= w.least_last;
+  return x;
+}
+
+// What one query row sees
+struct RowSight {
+  uint64_t bits;       // kSeeTree: of the new rows
+  int first, last;     // kSeeWindow
+  bool none;           // no key at all
+};
+
+template <int SEES>
+__device__ __forceinline__ RowSight sight_of(const PagedAttnParams& p, const PagedItem& w, int row) {
+  RowSight r;
+  r.bits = 0;
+  r.first = r.last = 0;
+  if (SEES == kSeeTree) {
+    const uint64_t there = w.count >= 64 ? ~0ull : (1ull << w.count) - 1;
+    r.bits = (p.mask ? p.mask[w.b * p.mask_stride + row] : ~0ull) & there;
+    r.none = w.length == 0 && r.bits == 0;
+  } else {
+    r.first = first_seen(p, w.length + row);
+    r.last = last_seen<SEES>(p, w.end, w.length + row);
+    r.none = r.last < 0 || (r.first > r.last && p.sinks == 0);
+  }
+  return r;
+}
+
+// Bits [a, b) of 32, for any a and b
+__device__ __forceinline__ uint32_t bits_between(int a, int b) {
+  a = min(max(a, 0), 32);
+  b = min(max(b, 0), 32);
+  const uint32_t below_b = b == 32 ? ~0u : (1u << b) - 1, below_a = a == 32 ? ~0u : (1u << a) - 1;
+  return below_b & ~below_a;
+}
+
+// Bit r: the row sees key r of the tile
+template <int SEES>
+__device__ __forceinline__ uint32_t seen_bits(const PagedAttnParams& p, const PagedTile& x, const RowSight& r) {
+  if (SEES == kSeeTree) return x.own ? (uint32_t)(r.bits >> x.at) : bits_between(0, x.hi);
+  const uint32_t upto = bits_between(0, r.last + 1 - x.at);
+  return upto & (bits_between(r.first - x.at, 32) | bits_between(0, p.sinks - x.at));
+}
+
+// The page that holds a row, one of the pool's in any case
+__device__ __forceinline__ int64_t page_of(const PagedCache& c, int b, int row) {
+  return min(max(c.table[b * c.table_stride + (row >> c.page_shift)], 0), c.n_pages - 1);
+}
+
+// Values of a masked tile that are no numbers take no part in rows that do not see them, where zero times them would be NaN.  They are left out of the
+// product; a second product of these codes with 1 for seen and 0 for unseen keys counts, per result, the seen +inf, -inf and NaN of up to 32 keys.
+__device__ __forceinline__ float special_code(float v) { return v != v ? 4096.f : v > 0.f ? 1.f : 64.f; }
+__device__ __forceinline__ float special_sum(float n) {
+  const int k = (int)n;
+  const bool nan = k >= 4096, plus = (k & 63) != 0, minus = (k & 4095) >= 64;
+  return nan || (plus && minus) ? __builtin_nanf("") : plus ? INFINITY : minus ? -INFINITY : 0.f;
+}
+
+}  // namespace sdllm

@@ -1,0 +1,171 @@
+// bf16 tiles of the paged cache in LDS, and what the matrix cores take of them: 32 keys by 32 query columns, fragments as in attn_tile_math.h (K rows as
+// the A operand of the logits, V columns through the transposing LDS read, P^T as the B operand), for head_dim 64 and 128.
+//
+// A tile of one tensor comes as HD / 16 fetches of 1 KB of consecutive LDS, each of whole rows in order; which 16-byte piece of its row a lane brings is free, so
+// the pieces of a row are permuted to keep the operand reads off each other's banks.
+#pragma once
+
+#include "attn_tile_math.h"
+#include "paged_tile.h"
+
+namespace sdllm {
+
+template <int HD>
+struct BfTile {
+  static constexpr int kRow = HD * 2, kBytes = kTileKeys * kRow;
+  static constexpr int kPieces = kRow / 16;             // of a row
+  static constexpr int kRowsPerFetch = kWave / kPieces;
+  static constexpr int kFetches = kTileKeys / kRowsPerFetch;
+  static constexpr int NP = HD / 16;                    // operands of the logits
+  static constexpr int NE = HD / 32;                    // accumulators
+  // row r holds piece c of K in place c ^ k_turn(r), of V in place c ^ v_turn(r)
+  static __device__ __forceinline__ int k_turn(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
+  static __device__ __forceinline__ int v_turn(int r) { return HD == 128 ? (r & 3) << 2 : (r & 2) << 1; }
+
+  struct Frags { i16x8 av[2][NE]; };
+
+  static __device__ __forceinline__ void read_k(const uint8_t* tile, int half, int col, bf16x8 (&a)[NP]) {
+    const uint32_t at = (uint32_t)(col * kRow + ((half ^ k_turn(col)) << 4));
+#pragma unroll
+    for (int i = 0; i < NP; ++i) a[i] = *reinterpret_cast<const bf16x8*>(tile + (at ^ (uint32_t)(i * 32)));
+  }
+  static __device__ __forceinline__ void read_v(const uint8_t* tile, int lane, Frags& f) {
+    typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+    const int half = lane >> 5, grp = (lane >> 4) & 1, s16 = lane & 15, r = half * 4 + (s16 >> 2);
+    const uint32_t at = (uint32_t)(r * kRow + ((v_turn(r) << 4) ^ (grp * 32 + (s16 & 3) * 8)));
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int e = 0; e < NE; ++e) {
+        const uint8_t* from = tile + (at ^ (uint32_t)(e * 64)) + st * 16 * kRow;
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)from);
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(from + 8 * kRow));
+        f.av[st][e] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+  }
+  static __device__ __forceinline__ void logits(const bf16x8 (&a)[NP], const bf16x8 (&qf)[NP], f32x16& s) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], qf[i], s, 0, 0, 0);
+  }
+  static __device__ __forceinline__ void pv(const Frags& f, const bf16x8 (&pb)[2], f32x16 (&acc)[NE]) {
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int e = 0; e < NE; ++e)
+        acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f.av[st][e]), pb[st], acc[e], 0, 0, 0);
+  }
+};
+
+// Logits of keys that a row does not see become -inf; `seen` is the row's bits of the tile (seen_bits).
+__device__ __forceinline__ void mask_logits(f32x16& s, uint32_t seen, int half) {
+  seen >>= 4 * half;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = seen >> (8 * (i >> 2) + (i & 3)) & 1 ? s[i] : -INFINITY;
+}
+
+// Softmax numerators of a tile's raw logits as the B operands of the second product, against a reference that moves when a maximum exceeds it by
+// more than kRescaleSlack (attn_tile_math.h).  Rounded to bf16, the type of what they multiply: half a step, 2^-8, of each numerator,
+// as much as the rounding of the result.
+template <int NE>
+__device__ __forceinline__ void numerators(f32x16& s, float scale_log2, float& m_ref, float& l_run, f32x16 (&acc)[NE], bf16x8 (&pb)[2]) {
+  float m_loc = s[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) m_loc = fmaxf(m_loc, s[i]);
+  m_loc *= scale_log2;
+  if (__ballot(m_loc > m_ref + kRescaleSlack) != 0) {
+    const float m_new = fmaxf(m_ref, fmaxf(m_loc, __shfl_xor(m_loc, 32)));
+    const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
+    m_ref = m_new;
+    l_run *= alpha;
+#pragma unroll
+    for (int e = 0; e < NE; ++e)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[e][i] *= alpha;
+  }
+  float l_loc = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale_log2, -m_ref));
+    l_loc += x;
+    pb[i >> 3][i & 7] = (__bf16)x;
+  }
+  l_run += l_loc;
+}
+
+// A masked tile's values that are no numbers (paged_tile.h): taken out of the operands, and what they make of the results added
+template <int HD>
+__device__ __forceinline__ void split_off_specials(typename BfTile<HD>::Frags& f, uint32_t seen, int half, f32x16 (&acc)[BfTile<HD>::NE]) {
+  constexpr int NE = BfTile<HD>::NE;
+  bool any = false;
+#pragma unroll
+  for (int st = 0; st < 2; ++st)
+#pragma unroll
+    for (int e = 0; e < NE; ++e)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) any |= (f.av[st][e][j] & 0x7f80) == 0x7f80;
+  if (__ballot(any) == 0) return;
+  seen >>= 4 * half;
+  bf16x8 one[2];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) one[i >> 3][i & 7] = (__bf16)(seen >> (8 * (i >> 2) + (i & 3)) & 1 ? 1.f : 0.f);
+#pragma unroll
+  for (int e = 0; e < NE; ++e) {
+    f32x16 sums;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sums[i] = 0.f;
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      bf16x8 codes;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const short v = f.av[st][e][j];
+        const bool special = (v & 0x7f80) == 0x7f80;
+        codes[j] = (__bf16)(special ? special_code((float)__builtin_bit_cast(__bf16, v)) : 0.f);
+        f.av[st][e][j] = special ? (short)0 : v;
+      }
+      sums = __builtin_amdgcn_mfma_f32_32x32x16_bf16(codes, one[st], sums, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[e][i] += special_sum(sums[i]);
+  }
+}
+
+// Where the rows of a tile are (bf16): rows 0-15 and 16-31 lie in one page each, or in the same.  Wave-uniform.
+struct TileBase { const char *k[2], *v[2]; uint32_t stride; int lo, hi; };
+
+// page[h]: page of the first row in half h that somebody sees
+template <int SEES>
+__device__ __forceinline__ TileBase tile_base(const PagedAttnParams& p, const PagedItem& w, const PagedTile& x, const int (&page)[2]) {
+  TileBase r;
+  r.lo = x.lo;
+  r.hi = x.hi;
+  if (SEES == kSeeTree && x.own) {
+    r.stride = (uint32_t)(p.blk_sr * 2);
+    const int64_t at = 2 * (w.b * p.blk_sb + w.g * p.blk_sh + x.at * p.blk_sr);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // rows of the second half that are not there are copies of the first's last
+      const int64_t half = h == 1 && x.hi > 16 ? 16 * (int64_t)r.stride : 0;
+      r.k[h] = (const char*)p.k_blk + at + half;
+      r.v[h] = (const char*)p.v_blk + at + half;
+    }
+    return r;
+  }
+  const PagedCache& c = p.cache;
+  r.stride = (uint32_t)(c.sr * 2);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int first = (x.at + min(max(16 * h, x.lo), x.hi - 1)) & ~15;
+    const int64_t at = 2 * (page[h] * c.sp + w.g * c.sh + (first & ((1 << c.page_shift) - 1)) * c.sr);
+    r.k[h] = (const char*)p.k_pages + at;
+    r.v[h] = (const char*)p.v_pages + at;
+  }
+  return r;
+}
+
+// Row of a half's page that stands at row r of the tile: itself, or the nearest that somebody sees
+__device__ __forceinline__ uint32_t row_in_half(const TileBase& t, int r) { return (uint32_t)(min(max(r, t.lo), t.hi - 1) & 15); }
+
+}  // namespace sdllm

@@ -209,6 +209,60 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
+PyObject* append_paged(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count_is(n, 18)) return nullptr;
+  Args a{args};
+  const auto f = reinterpret_cast<decltype(&sdllm_append_paged)>(a.address());
+  const auto* qk = static_cast<const sdllm_qk_shape_t*>(a.address());
+  const auto* shape = static_cast<const sdllm_paged_shape_t*>(a.address());
+  void *q = a.tensor(), *k = a.tensor(), *v = a.tensor(), *qw = a.tensor(), *kw = a.tensor(), *freq = a.tensor(), *pos = a.tensor(), *pick = a.tensor();
+  void *lengths = a.tensor(), *counts = a.tensor(), *table = a.tensor(), *qo = a.tensor(), *kp = a.tensor(), *vp = a.tensor(), *stream = a.address();
+  if (!a.ok) return nullptr;
+  using Ints = const int32_t*;
+  int32_t status;
+  Py_BEGIN_ALLOW_THREADS
+  status = f(qk, shape, q, k, v, qw, kw, static_cast<const float*>(freq), static_cast<Ints>(pos), static_cast<Ints>(pick), static_cast<Ints>(lengths),
+             static_cast<Ints>(counts), static_cast<Ints>(table), qo, kp, vp, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+PyObject* tree_attn_paged(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count_is(n, 14)) return nullptr;
+  Args a{args};
+  const auto f = reinterpret_cast<decltype(&sdllm_tree_attn_paged)>(a.address());
+  const auto* shape = static_cast<const sdllm_paged_shape_t*>(a.address());
+  void *q = a.tensor(), *kp = a.tensor(), *vp = a.tensor(), *table = a.tensor(), *lengths = a.tensor(), *counts = a.tensor();
+  void *kb = a.tensor(), *vb = a.tensor(), *mask = a.tensor(), *out = a.tensor();
+  const size_t ws_bytes = a.bytes();
+  void *ws = a.tensor(), *stream = a.address();
+  if (!a.ok) return nullptr;
+  using Ints = const int32_t*;
+  int32_t status;
+  Py_BEGIN_ALLOW_THREADS
+  status = f(shape, q, kp, vp, static_cast<Ints>(table), static_cast<Ints>(lengths), static_cast<Ints>(counts), kb, vb,
+             static_cast<const uint64_t*>(mask), out, ws, ws_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+PyObject* window_attn_paged(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count_is(n, 11)) return nullptr;
+  Args a{args};
+  const auto f = reinterpret_cast<decltype(&sdllm_window_attn_paged)>(a.address());
+  const auto* shape = static_cast<const sdllm_paged_shape_t*>(a.address());
+  void *q = a.tensor(), *kp = a.tensor(), *vp = a.tensor(), *table = a.tensor(), *lengths = a.tensor(), *counts = a.tensor(), *out = a.tensor();
+  const size_t ws_bytes = a.bytes();
+  void *ws = a.tensor(), *stream = a.address();
+  if (!a.ok) return nullptr;
+  using Ints = const int32_t*;
+  int32_t status;
+  Py_BEGIN_ALLOW_THREADS
+  status = f(shape, q, kp, vp, static_cast<Ints>(table), static_cast<Ints>(lengths), static_cast<Ints>(counts), out, ws, ws_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
 template <class F>
 PyCFunction fast(F* f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
@@ -221,6 +275,11 @@ PyMethodDef methods[] = {
     {"compact_packed", fast(compact_packed), METH_FASTCALL, "function, shape, k, v, idx, cache, cache_rows, stream"},
     {"unpack_kv", fast(unpack_kv), METH_FASTCALL, "function, shape, cache, cache_rows, n_cached, k, v, stream"},
     {"qk_norm_rope", fast(qk_norm_rope), METH_FASTCALL, "function, shape, q, k, q_weight, k_weight, inv_freq, positions, q_out, k_out, stream"},
+    {"append_paged", fast(append_paged), METH_FASTCALL,
+     "function, qk shape, shape, q, k, v, q_weight, k_weight, inv_freq, positions, pick, lengths, row_counts, table, q_out, k_pages, v_pages, stream"},
+    {"tree_attn_paged", fast(tree_attn_paged), METH_FASTCALL,
+     "function, shape, q, k_pages, v_pages, table, lengths, row_counts, k, v, mask, out, ws, stream"},
+    {"window_attn_paged", fast(window_attn_paged), METH_FASTCALL, "function, shape, q, k_pages, v_pages, table, lengths, row_counts, out, ws, stream"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,27 +1,15 @@
 // Norm of each query and key head and rotation by position in one pass: what turns a projection into the q_blk and k_in of a block
 // step.  y = x / sqrt(mean(x^2) + eps) * w per head, then each pair (a, b) of frequency f becomes (a cos t - b sin t, a sin t + b cos t), t =
-// position * inv_freq[f].  fp32 throughout, one rounding at the end; t in 64 bits, reduced to a part of a turn, because 32 bits leave of an angle of
-// 10^5 no more than 2^-7, and what rounding that part to 32 bits leaves off goes into its sine and cosine.
+// position * inv_freq[f].  fp32 throughout, one rounding at the end; t in 64 bits (qk_rope_math.h, which has the arithmetic).
 //
-// Bound by memory.  A lane holds the two 16-byte pieces of a head that are turned into each other, 4 to 16 lanes a head, and a wavefront
-// 4 to 16 heads of one position, so that an angle is computed once by one lane and handed to the others.
-#include "mfma_tile.h"
+// Bound by memory.
+#include "qk_rope_math.h"
 
 namespace sdllm {
 
 namespace {
 
 constexpr int kRopeThreads = 256;   // at most
-
-template <typename T> struct Piece;
-template <> struct Piece<__bf16> { using Vec = bf16x8; static constexpr int N = 8; };
-template <> struct Piece<float> { using Vec = f32x4; static constexpr int N = 4; };
-
-template <bool NT, class V> __device__ __forceinline__ V read(const V* at) { return NT ? __builtin_nontemporal_load(at) : *at; }
-template <bool NT, class V> __device__ __forceinline__ void write(const V& v, V* at) {
-  if constexpr (NT) __builtin_nontemporal_store(v, at);
-  else *at = v;
-}
 
 template <typename T, int HD, bool NT>
 __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(const QkParams p) {
@@ -36,31 +24,16 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(const QkPara
   const int b = p.by_rows.quotient(token), row = token - b * p.rows;
   const int sub = lane % kLanes, slot = lane / kLanes;
 
-  // one angle per lane
-  const int freqs = p.rot >> 1;
-  float cs = 1.f, sn = 0.f;
-  if (lane < freqs) {
-    const int position = p.positions ? p.positions[b * p.pos_stride + row] : p.pos_begin + row;
-    double turns = (double)position * (double)p.inv_freq[lane] * 0.15915494309189533577;
-    turns -= rint(turns);
-    // in half turns, as a float and what that leaves off: sine and cosine of their sum, to first order
-    const double half_turns = 2.0 * turns;
-    const float near = (float)half_turns, rest = 3.14159265f * (float)(half_turns - (double)near);
-    float s0, c0;
-    sincospif(near, &s0, &c0);
-    sn = __builtin_fmaf(c0, rest, s0);
-    cs = __builtin_fmaf(-s0, rest, c0);
-  }
+  const int position = p.rot == 0 ? 0 : p.positions ? p.positions[b * p.pos_stride + row] : p.pos_begin + row;
+  float cs, sn;
+  lane_angle(position, p.inv_freq, lane, p.rot >> 1, cs, sn);
   float c[N], s[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     c[i] = __shfl(cs, sub * N + i);
     s[i] = __shfl(sn, sub * N + i);
   }
-  // pieces: the two halves of the turned channels, then what is left in order; or neighbours
-  const int half = p.rot / (2 * N);
-  const bool turned = sub < half;
-  const int first = (p.adjacent || !turned ? 2 * sub : sub) * N, second = (p.adjacent || !turned ? 2 * sub + 1 : sub + half) * N;
+  const auto [first, second, turned] = pieces_of(sub, p.rot, p.adjacent, N);
 
   const int heads = p.hq + p.hkv;
   for (int h0 = part * kHeads; h0 < heads; h0 += p.parts * kHeads) {
@@ -70,68 +43,22 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(const QkPara
     float x[2 * N];
     if (there) {
       const T* src = is_q ? (const T*)p.q_in + b * p.qi_sb + hh * p.qi_sh + row * p.qi_sr : (const T*)p.k_in + b * p.ki_sb + hh * p.ki_sh + row * p.ki_sr;
-      const Vec u = read<NT>(reinterpret_cast<const Vec*>(src + first)), v = read<NT>(reinterpret_cast<const Vec*>(src + second));
+      const Vec u = read_piece<NT>(reinterpret_cast<const Vec*>(src + first)), v = read_piece<NT>(reinterpret_cast<const Vec*>(src + second));
 #pragma unroll
       for (int i = 0; i < N; ++i) { x[i] = (float)u[i]; x[N + i] = (float)v[i]; }
     } else {
 #pragma unroll
       for (int i = 0; i < 2 * N; ++i) x[i] = 0.f;
     }
-    if (p.norm) {
-      // mean(x^2) + eps, with eps f^2 for rows that were multiplied by f
-      auto mean_square = [&](float eps) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 2 * N; ++i) sum = __builtin_fmaf(x[i], x[i], sum);
-#pragma unroll
-        for (int o = 1; o < kLanes; o <<= 1) sum += __shfl_xor(sum, o);
-        return __builtin_fmaf(sum, 1.f / HD, eps);
-      };
-      float ms = mean_square(p.eps);
-      // Rows whose squares are not numbers of fp32, or are so small that they lose bits, are brought near 1 by a power of two first: elements up to
-      // 2^128 become 2^58, ones below 2^-41 up to 2^59.  All lanes go in for one row, the others with a factor of 1.  The test is 0.05 of 2.9 us for a
-      // block's rows.
-      if (__ballot(!(ms >= 0x1p-90f && ms <= 0x1p120f)) != 0) {
-        const float f = ms >= 0x1p-90f ? ms <= 0x1p120f ? 1.f : 0x1p-70f : 0x1p100f;
-#pragma unroll
-        for (int i = 0; i < 2 * N; ++i) x[i] *= f;
-        ms = mean_square(p.eps * f * f);
-      }
-      const float r = 1.f / sqrtf(ms);
-      const T* w = (const T*)(is_q ? p.q_weight : p.k_weight);
-      if (w) {
-        const Vec u = *reinterpret_cast<const Vec*>(w + first), v = *reinterpret_cast<const Vec*>(w + second);
-#pragma unroll
-        for (int i = 0; i < N; ++i) { x[i] = x[i] * r * (float)u[i]; x[N + i] = x[N + i] * r * (float)v[i]; }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 2 * N; ++i) x[i] *= r;
-      }
-    }
-    if (turned) {
-      if (p.adjacent) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float a = x[2 * i], bb = x[2 * i + 1];
-          x[2 * i] = a * c[i] - bb * s[i];
-          x[2 * i + 1] = a * s[i] + bb * c[i];
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float a = x[i], bb = x[N + i];
-          x[i] = a * c[i] - bb * s[i];
-          x[N + i] = a * s[i] + bb * c[i];
-        }
-      }
-    }
+    if (p.norm) norm_head<T, HD>(x, (const T*)(is_q ? p.q_weight : p.k_weight), first, second, p.eps);
+    if (turned) turn_pairs<N>(x, c, s, p.adjacent);
     if (there) {
       T* dst = is_q ? (T*)p.q_out + b * p.qo_sb + hh * p.qo_sh + row * p.qo_sr : (T*)p.k_out + b * p.ko_sb + hh * p.ko_sh + row * p.ko_sr;
       Vec u, v;
 #pragma unroll
       for (int i = 0; i < N; ++i) { u[i] = (T)x[i]; v[i] = (T)x[N + i]; }
-      write<NT>(u, reinterpret_cast<Vec*>(dst + first));
-      write<NT>(v, reinterpret_cast<Vec*>(dst + second));
+      write_piece<NT>(u, reinterpret_cast<Vec*>(dst + first));
+      write_piece<NT>(v, reinterpret_cast<Vec*>(dst + second));
     }
   }
 }

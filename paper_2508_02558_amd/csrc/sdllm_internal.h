@@ -292,11 +292,68 @@ struct QkParams {
   Divisor by_rows;
 };
 
+// ---- the paged cache
+constexpr int kPagedMax = 1 << 29;    // most rows of a sequence, old or new: places, limits of windows and their sums are 32-bit integers
+
+// Where the rows of the sequences are
+struct PagedCache {
+  const int32_t* table;
+  const int32_t* lengths;
+  const int32_t* counts;              // null: `rows` each
+  int64_t table_stride;
+  int64_t sp, sh, sr;                 // strides of the pages: page, head, row, in elements
+  int32_t n_pages, page_shift;        // page_rows = 1 << page_shift
+  int32_t capacity;                   // rows that a sequence can have, 0 if there are no pages
+  int32_t rows;                       // new rows, at most
+
+  __device__ int length(int b) const { return min(max(lengths[b], 0), capacity); }
+  __device__ int count(int b) const { return counts ? min(max(counts[b], 0), rows) : rows; }
+};
+
+struct AppendParams {
+  QkParams qk;                        // k_out strides and `rows` unread
+  PagedCache cache;
+  const void* v_in;
+  const int32_t* pick;
+  void* k_pages;
+  void* v_pages;
+};
+
+enum { kSeeTree = 0, kSeeWindow = 1 };
+struct PagedAttnParams {
+  PagedCache cache;
+  const void* q;
+  const void* k_pages;
+  const void* v_pages;
+  const void* k_blk;                  // kSeeTree
+  const void* v_blk;
+  const uint64_t* mask;
+  void* out;
+  int64_t mask_stride;
+  int64_t q_sb, q_sh, q_sr, blk_sb, blk_sh, blk_sr, o_sb, o_sh, o_sr;   // in elements
+  int32_t batch, hkv, group;
+  int32_t left, right, sinks;         // kSeeWindow; left or right negative: no limit
+  float scale_log2;
+  // plan (plan_paged): what a workgroup takes is found on the device from the lengths
+  int32_t block_cols, max_blocks;     // query columns of a workgroup; blocks of them that a KV head has at most
+  int32_t workgroups, least_tiles;    // of the launch; 32-key tiles below which a workgroup's share is not cut
+  float* part_o;                      // [workgroups][block_cols][d]; null: nothing is split, workgroups are the items
+  float* part_ml;                     // [workgroups][2][block_cols]
+  int32_t* item_at;                   // [batch x hkv x max_blocks][2]: first of an item's workgroups in part_*, how many
+  Divisor by_group, by_blocks, by_hkv;
+};
+
 // Most wavefronts of a workgroup: with fp32 tensors the three parts of the queries take the registers of two
 constexpr int kPackedWavesBf16 = 8, kPackedWavesF32 = 4;
 hipError_t launch_pack(const PackParams& p, int dtype, int d, hipStream_t s);
 hipError_t launch_unpack(const PackParams& p, int dtype, int d, hipStream_t s);
 hipError_t launch_attn_packed(const PackedAttnParams& p, int dtype, int d, hipStream_t s);
 hipError_t launch_qk_norm_rope(const QkParams& p, int dtype, int d, hipStream_t s);
+hipError_t launch_append_paged(const AppendParams& p, int dtype, int d, hipStream_t s);
+// how a call is cut up; pl of a launch or of the host's question
+struct PagedPlan { int kernel, block_cols, waves, max_blocks, workgroups, least_tiles; bool splits; };
+hipError_t launch_attn_paged(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
+hipError_t launch_attn_paged_f32(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
+hipError_t launch_attn_paged_stream(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
 
 }  // namespace sdllm
