@@ -99,6 +99,7 @@ __global__ __launch_bounds__(kGeneralMaxWaves * kWave) void attn_paged_f32_kerne
   for (int e = 0; e < O::NE; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = kNoMax, l_run = 0.f;      // softmax reference of the row; sum over the keys this lane has seen
 
+  bool specials = false;                  // values of masked tiles that are no numbers
   int t = t_begin + wave;
   PagedTile next;
   TileRows rows;
@@ -120,11 +121,10 @@ __global__ __launch_bounds__(kGeneralMaxWaves * kWave) void attn_paged_f32_kerne
     }
     float s[NS];
     O::logits(lds_k, qf, col, part, s);
-    uint32_t seen = 0;
     if (!x.full) {
-      seen = seen_bits<SEES>(p, x, sight) >> (4 * part);
+      const uint32_t seen = seen_bits<SEES>(p, x, sight) >> (4 * part);
 #pragma unroll
-      for (int i = 0; i < NS; ++i) s[i] = seen >> O::key(i, 0) & 1 ? s[i] : -INFINITY;
+      for (int i = 0; i < NS; ++i) s[i] = or_minus_infinity(s[i], bit_mask(seen, O::key(i, 0)));
     }
     float m_loc = s[0];
 #pragma unroll
@@ -148,37 +148,23 @@ __global__ __launch_bounds__(kGeneralMaxWaves * kWave) void attn_paged_f32_kerne
     }
     l_run += l_loc;
     if (!x.full) {
-      bool special = false;
+      // bit 31: exponent all ones
+      auto special = [](float v) { return (__builtin_bit_cast(uint32_t, v) & 0x7f800000u) + 0x00800000u & 0x80000000u; };
+      uint32_t any = 0;
 #pragma unroll
       for (int i = 0; i < NS; ++i)
 #pragma unroll
         for (int c = 0; c < O::NE / 4; ++c)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) special |= !(fabsf(vreg.r[i][c][k]) < INFINITY);
-      if (__ballot(special)) {
-        typename O::V codes;
-        float one[NS];
-        typename O::Acc sums[O::NE];
+          for (int k = 0; k < 4; ++k) any |= special(vreg.r[i][c][k]);
+      if (__ballot(any != 0)) {
+        specials = true;
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-          one[i] = seen >> O::key(i, 0) & 1 ? 1.f : 0.f;
+        for (int i = 0; i < NS; ++i)
 #pragma unroll
           for (int c = 0; c < O::NE / 4; ++c)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float v = vreg.r[i][c][k];
-              const bool finite = fabsf(v) < INFINITY;
-              codes.r[i][c][k] = finite ? 0.f : special_code(v);
-              vreg.r[i][c][k] = finite ? v : 0.f;
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < O::NE; ++e) sums[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-        g_pv<D>(lds_k, codes, one, lane, sums);
-#pragma unroll
-        for (int e = 0; e < O::NE; ++e)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[e][i] += special_sum(sums[e][i]);
+            for (int k = 0; k < 4; ++k) vreg.r[i][c][k] = special(vreg.r[i][c][k]) ? 0.f : vreg.r[i][c][k];
       }
     }
     g_pv<D>(lds_k, vreg, s, lane, acc);
@@ -187,6 +173,16 @@ __global__ __launch_bounds__(kGeneralMaxWaves * kWave) void attn_paged_f32_kerne
     __builtin_amdgcn_wave_barrier();
   }
 
+  if (specials)
+    add_specials<SEES>(p, w, sight, 4, 0, ceil_div(t_end - t_begin - wave, nw), [&](int n) { return t_begin + wave + n * nw; }, [&](const char* v, bool sees) {
+#pragma unroll
+      for (int e = 0; e < O::NE; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float z = reinterpret_cast<const float*>(v)[64 * (e >> 2) + 4 * (4 * part + i) + (e & 3)];
+          acc[e][i] += sees && !(fabsf(z) < INFINITY) ? z : 0.f;
+        }
+    });
   // merge of the waves: each parks its results ([lane][unit of four columns]) and its rows' statistics
   const float l_tot = parts_sum<O>(l_run);
   uint8_t* mine = smem + wave * kWaveBytes;

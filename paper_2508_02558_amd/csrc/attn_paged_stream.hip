@@ -37,30 +37,31 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   const int row = p.by_group.quotient(in), head = w.g * p.group + in - row * p.group;
   const RowSight sight = sight_of<SEES>(p, w, row);
 
+  const ItemBase item = item_base<SEES>(p, w);
   // pages of tiles 64 i .. 64 i + 63 of this wavefront's, one per lane
   int pages[2] = {0, 0};
-  auto look_up = [&](int j0) {
+  auto look_up = [&](int j0) __attribute__((always_inline)) {
     const int t = min(t_begin + (j0 + lane) * nw, w.tiles - 1);
     const PagedTile x = tile_of<SEES>(p, w, t);
     if (SEES == kSeeTree && x.own) return;
 #pragma unroll
     for (int h = 0; h < 2; ++h) pages[h] = (int)page_of(p.cache, w.b, x.at + min(max(16 * h, x.lo), x.hi - 1));
   };
-  auto base_of = [&](int j, PagedTile& x) {
+  auto base_of = [&](int j, PagedTile& x) __attribute__((always_inline)) {
     x = tile_of<SEES>(p, w, t_begin + j * nw);
     const int page[2] = {__builtin_amdgcn_readlane(pages[0], j & 63), __builtin_amdgcn_readlane(pages[1], j & 63)};
-    return tile_base<SEES>(p, w, x, page);
+    return tile_base<SEES>(item, x, page);
   };
 
   uint8_t* k_lds = smem + wave * kWaveLds;
   uint8_t* v_lds = k_lds + T::kBytes;
   const int r0 = lane / T::kPieces, place = lane % T::kPieces;
-  auto fetch = [&](const TileBase& t, bool is_v, uint8_t* lds) {
+  auto fetch = [&](const TileBase& t, bool is_v, uint8_t* lds) __attribute__((always_inline)) {
     const uint32_t to = lds_address(lds);
 #pragma unroll
     for (int j = 0; j < T::kFetches; ++j) {
       const int r = j * T::kRowsPerFetch + r0, h = j * T::kRowsPerFetch >> 4;
-      const char* base = is_v ? t.v[h] : t.k[h];
+      const char* base = (t.own ? is_v ? item.v_own : item.k_own : is_v ? item.v : item.k) + t.at[h];
       const uint32_t piece = (uint32_t)(place ^ (is_v ? T::v_turn(r) : T::k_turn(r))) << 4;
       fetch_to_lds(to + (uint32_t)j * 1024, in_scalars(base), row_in_half(t, r) * t.stride + piece);
     }
@@ -73,23 +74,22 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
     for (int i = 0; i < 16; ++i) acc[e][i] = 0.f;
   float m_run = kNoMax, l_run = 0.f;
   bf16x8 qf[T::NP], a[T::NP], pb[2];
-  typename T::Frags f;
+  i16x8 f[2 * NE];
   f32x16 s;
 
   // Requests in order: K(0), V(0), K(1), and then for each tile j K(j+2), V(j+1).  The waits count them.  Loads by the compiler in between (pages)
   // make a wait longer, never shorter.
   PagedTile x, x_next;
   TileBase base_next;
-  auto landed = [&](bool all) {
+  auto landed = [&](bool all) __attribute__((always_inline)) {
     if (all) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     else if constexpr (T::kFetches == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
     wave_lds_sync();
   };
-  uint32_t seen = ~0u;
-  bool full = true;
+  bool full = true, specials = false;   // of the tile whose second product is next; values of masked tiles that are no numbers
   // logits of tile j, then the next K
-  auto logits = [&](int j) {
+  auto logits = [&](int j) __attribute__((always_inline)) {
     x = x_next;
     T::read_k(k_lds, half, col, a);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -101,54 +101,49 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
     in_issue_order();
     T::logits(a, qf, s);
   };
-  auto softmax = [&]() {
+  auto softmax = [&]() __attribute__((always_inline)) {
     full = x.full;
-    if (!full) {
-      seen = seen_bits<SEES>(p, x, sight);
-      mask_logits(s, seen, half);
-    }
+    if (!full) mask_logits(s, seen_bits<SEES>(p, x, sight), half);
     numerators<NE>(s, p.scale_log2, m_run, l_run, acc, pb);
   };
-  auto product = [&]() {
-    if (!full) split_off_specials<HD>(f, seen, half, acc);
-    T::pv(f, pb, acc);
-  };
-
   if (n_mine > 0) {
     look_up(0);
-    TileBase base = base_of(0, x_next);
-    fetch(base, false, k_lds);
+    TileBase base_v = base_of(0, x_next);
+    fetch(base_v, false, k_lds);
     in_issue_order();
-    fetch(base, true, v_lds);
+    fetch(base_v, true, v_lds);
     in_issue_order();
     const u32x4* q = reinterpret_cast<const u32x4*>((const char*)p.q + 2 * (w.b * p.q_sb + head * p.q_sh + row * p.q_sr));
 #pragma unroll
     for (int i = 0; i < T::NP; ++i) qf[i] = __builtin_bit_cast(bf16x8, q[i * 2 + half]);
-    landed(true);
-    logits(0);
-    softmax();
-    for (int j = 0; j + 1 < n_mine; ++j) {
-      const TileBase base_v = base_next;    // of tile j + 1
-      landed(j == 0);                       // K(j+1); V(j) may still fly
-      logits(j + 1);
-      landed(j + 2 >= n_mine);              // V(j); K(j+2), if there is one, may still fly
-      T::read_v(v_lds, lane, f);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      fetch(base_v, true, v_lds);
-      in_issue_order();
-      product();
-      __builtin_amdgcn_sched_barrier(0);
-      softmax();
+    // logits of tile j, second product of tile j - 1, softmax of tile j
+    for (int j = 0; j <= n_mine; ++j) {
+      if (j < n_mine) {
+        if (j > 0) base_v = base_next;
+        landed(j <= 1);                     // K(j); V(j-1) may still fly
+        logits(j);
+      }
+      if (j > 0) {
+        landed(j + 1 >= n_mine);            // V(j-1); K(j+1), if there is one, may still fly
+        T::read_v(v_lds, lane, f);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (j < n_mine) fetch(base_v, true, v_lds);
+        in_issue_order();
+        if (!full) specials |= take_specials(f);
+        T::pv(f, pb, acc);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (j < n_mine) softmax();
     }
-    landed(true);
-    T::read_v(v_lds, lane, f);
-    product();
   }
 
+  if (specials)
+    add_specials<SEES>(p, w, sight, 2, 0, n_mine, [&](int j) { return t_begin + j * nw; },
+                       [&](const char* v, bool sees) __attribute__((always_inline)) { add_special_row<NE>(v, sees, half, acc); });
   const float l_tot = l_run + __shfl_xor(l_run, 32);
   // Merge: every wavefront parks its accumulators (slot i of a lane in place i ^ its turn) and its columns' statistics; they then share out the slots.
   auto turn = [](int l) { return HD == 128 ? l & 15 : (l >> 1) & 7; };
-  auto stat_of = [&](int k) { return reinterpret_cast<float*>(smem + k * kWaveLds + 2 * T::kBytes); };
+  auto stat_of = [&](int k) __attribute__((always_inline)) { return reinterpret_cast<float*>(smem + k * kWaveLds + 2 * T::kBytes); };
 #pragma unroll
   for (int e = 0; e < NE; ++e)
 #pragma unroll

@@ -46,15 +46,15 @@ int32_t fill_cache(const sdllm_paged_shape_t& s, const void* k_pages, const void
   return SDLLM_OK;
 }
 
-enum { kPagedF32 = 0, kPagedStream = 1 };
+enum { kPagedF32 = 0, kPagedStream = 1, kPagedShared = 2 };
 
 // How a call is cut up (paged_tile.h): columns of a workgroup by the kernel, and how many workgroups there are for shares of the tiles.
 int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   const int64_t cols = (int64_t)s.rows * (s.n_q_heads / s.n_kv_heads);
   pl = PagedPlan{};
-  pl.kernel = s.dtype == SDLLM_F32 ? kPagedF32 : kPagedStream;
-  pl.block_cols = pl.kernel == kPagedF32 ? kGeneralRowsF32 : 32;
-  pl.waves = pl.kernel == kPagedF32 ? kGeneralMaxWaves : 4;
+  pl.kernel = s.dtype == SDLLM_F32 ? kPagedF32 : cols <= 32 ? kPagedStream : kPagedShared;
+  pl.block_cols = pl.kernel == kPagedF32 ? kGeneralRowsF32 : pl.kernel == kPagedStream ? 32 : cols <= 128 ? 128 : 256;
+  pl.waves = pl.kernel == kPagedStream ? 4 : kGeneralMaxWaves;
   // columns, blocks and threads of a launch (the merge's too) are counted in 32 bits
   if (cols > INT32_MAX - 256) return SDLLM_ERR_UNSUPPORTED;
   pl.max_blocks = (int)((cols + pl.block_cols - 1) / pl.block_cols);
@@ -68,9 +68,11 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   if (tree) tiles += 2;
   else if (s.window_left >= 0 && s.window_right >= 0)
     tiles = std::min<int64_t>(tiles, ((int64_t)s.window_left + s.window_right + pl.block_cols) / kTileKeys + 2 + std::min(s.sinks, capacity) / kTileKeys);
-  pl.least_tiles = 8;
-  pl.splits = items <= 1024 && tiles > pl.least_tiles;
-  pl.workgroups = pl.splits ? (int)std::max<int64_t>(2 * kNumCUs, 2 * items) : (int)items;
+  // workgroups that the CUs hold at once
+  const int64_t at_once = pl.kernel == kPagedShared ? kNumCUs : 2 * kNumCUs;
+  pl.least_tiles = pl.kernel == kPagedShared ? 16 : 8;
+  pl.splits = items <= 2 * at_once && tiles > pl.least_tiles;
+  pl.workgroups = pl.splits ? (int)std::max<int64_t>(at_once, 2 * items) : (int)items;
   return SDLLM_OK;
 }
 
@@ -129,7 +131,9 @@ int32_t run_paged(const sdllm_paged_shape_t* shape, bool tree, const void* q, co
 }  // namespace
 
 hipError_t sdllm::launch_attn_paged(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s) {
-  return pl.kernel == kPagedF32 ? launch_attn_paged_f32(p, pl, sees, d, s) : launch_attn_paged_stream(p, pl, sees, d, s);
+  return pl.kernel == kPagedF32      ? launch_attn_paged_f32(p, pl, sees, d, s)
+         : pl.kernel == kPagedStream ? launch_attn_paged_stream(p, pl, sees, d, s)
+                                     : launch_attn_paged_shared(p, pl, sees, d, s);
 }
 
 extern "C" {

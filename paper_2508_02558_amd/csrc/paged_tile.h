@@ -74,7 +74,6 @@ __device__ __forceinline__ void locate_item(const PagedAttnParams& p, PagedItem&
 // The item and split of this workgroup, the same for all of its threads; false: none
 template <int SEES>
 __device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, PagedItem& w) {
-  int t_most;
   if (!p.part_o) {
     // Items as workgroups, the last block of a head first: with all past keys to see it has the most tiles
     const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
@@ -82,9 +81,9 @@ __device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, Pa
     w.blk = p.max_blocks - 1 - (id - head * p.max_blocks);
     w.b = p.by_hkv.quotient(head);
     w.g = head - w.b * p.hkv;
-    w.count = p.cache.count(w.b);
+    w.count = __builtin_amdgcn_readfirstlane(p.cache.count(w.b));
     if (w.blk * p.block_cols >= w.count * p.group) return false;
-    w.length = p.cache.length(w.b);
+    w.length = __builtin_amdgcn_readfirstlane(p.cache.length(w.b));
     w.split = 0;
     w.n_split = 1;
     w.slot = 0;
@@ -111,16 +110,16 @@ __device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, Pa
     items += p.hkv * s.blocks;
     tiles += (double)(p.hkv * s.blocks) * s.tiles;
   }
-  items = sum(items);
+  items = __builtin_amdgcn_readfirstlane(sum(items));
   tiles = sum(tiles);
   // the host launches more workgroups than there can be items
-  const int share = max(p.least_tiles, (int)ceil(tiles / max(1, p.workgroups - items)));
+  const int share = __builtin_amdgcn_readfirstlane(max(p.least_tiles, (int)ceil(tiles / max(1, p.workgroups - items))));
   int used = 0;
   for (int b0 = 0; b0 < p.batch; b0 += kWave) {
     const Seq s = sequence_at(b0);
     used += p.hkv * s.blocks * max(1, ceil_div(s.tiles, share));
   }
-  used = sum(used);
+  used = __builtin_amdgcn_readfirstlane(sum(used));
   if ((int)blockIdx.x >= used) return false;
   const int id = xcd_contiguous_id(blockIdx.x, used);
   int before = 0;
@@ -146,8 +145,8 @@ __device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, Pa
       w.g = unit / w.n_split;
       w.split = unit - w.g * w.n_split;
       w.slot = before + (w.g * blocks + w.blk) * w.n_split + w.split;
-      w.count = p.cache.count(w.b);
-      w.length = p.cache.length(w.b);
+      w.count = __builtin_amdgcn_readfirstlane(p.cache.count(w.b));
+      w.length = __builtin_amdgcn_readfirstlane(p.cache.length(w.b));
       locate_item<SEES>(p, w);
       if (w.split == 0 && threadIdx.x == 0) {
         int32_t* at = p.item_at + 2 * ((int64_t)(w.b * p.hkv + w.g) * p.max_blocks + w.blk);
@@ -234,13 +233,32 @@ __device__ __forceinline__ int64_t page_of(const PagedCache& c, int b, int row) 
   return min(max(c.table[b * c.table_stride + (row >> c.page_shift)], 0), c.n_pages - 1);
 }
 
-// Values of a masked tile that are no numbers take no part in rows that do not see them, where zero times them would be NaN.  They are left out of the
-// product; a second product of these codes with 1 for seen and 0 for unseen keys counts, per result, the seen +inf, -inf and NaN of up to 32 keys.
-__device__ __forceinline__ float special_code(float v) { return v != v ? 4096.f : v > 0.f ? 1.f : 64.f; }
-__device__ __forceinline__ float special_sum(float n) {
-  const int k = (int)n;
-  const bool nan = k >= 4096, plus = (k & 63) != 0, minus = (k & 4095) >= 64;
-  return nan || (plus && minus) ? __builtin_nanf("") : plus ? INFINITY : minus ? -INFINITY : 0.f;
+// Bit `bit` of x as a mask of all bits: one instruction, and no comparison whose result would take a pair of scalar registers
+__device__ __forceinline__ uint32_t bit_mask(uint32_t x, int bit) { return (uint32_t)((int32_t)(x << (31 - bit)) >> 31); }
+__device__ __forceinline__ float or_minus_infinity(float s, uint32_t m) {
+  return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, s) & m) | (0xff800000u & ~m));
+}
+
+// Values of a masked tile that are no numbers take no part in rows that do not see them, where zero times them would be NaN.  They are taken out of the
+// operands, and a wavefront that met any goes over its masked tiles once more at the end, key by key, and adds them to the results of the rows that see
+// them: to find out costs masked tiles three instructions a pair of values, the rest nothing but where it happens.
+// `where(t)` is tile t of this wavefront's, `add(v_row, sees)` adds the infinities and NaN of one row of V.
+template <int SEES, class Where, class Add>
+__device__ __forceinline__ void add_specials(const PagedAttnParams& p, const PagedItem& w, const RowSight& sight, int esize, int first, int end, const Where& where,
+                                             const Add& add) {
+  const PagedCache& c = p.cache;
+  for (int n = first; n < end; ++n) {
+    const PagedTile x = tile_of<SEES>(p, w, where(n));
+    if (x.full) continue;
+    const uint32_t seen = seen_bits<SEES>(p, x, sight);
+    for (int r = x.lo; r < x.hi; ++r) {
+      const int row = x.at + r;
+      const char* v = SEES == kSeeTree && x.own
+                          ? (const char*)p.v_blk + esize * (w.b * p.blk_sb + w.g * p.blk_sh + row * p.blk_sr)
+                          : (const char*)p.v_pages + esize * (page_of(c, w.b, row) * c.sp + w.g * c.sh + (row & ((1 << c.page_shift) - 1)) * c.sr);
+      add(v, (seen >> r & 1) != 0);
+    }
+  }
 }
 
 }  // namespace sdllm

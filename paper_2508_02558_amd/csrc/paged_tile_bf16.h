@@ -22,14 +22,12 @@ struct BfTile {
   static __device__ __forceinline__ int k_turn(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
   static __device__ __forceinline__ int v_turn(int r) { return HD == 128 ? (r & 3) << 2 : (r & 2) << 1; }
 
-  struct Frags { i16x8 av[2][NE]; };
-
   static __device__ __forceinline__ void read_k(const uint8_t* tile, int half, int col, bf16x8 (&a)[NP]) {
     const uint32_t at = (uint32_t)(col * kRow + ((half ^ k_turn(col)) << 4));
 #pragma unroll
     for (int i = 0; i < NP; ++i) a[i] = *reinterpret_cast<const bf16x8*>(tile + (at ^ (uint32_t)(i * 32)));
   }
-  static __device__ __forceinline__ void read_v(const uint8_t* tile, int lane, Frags& f) {
+  static __device__ __forceinline__ void read_v(const uint8_t* tile, int lane, i16x8 (&f)[2 * NE]) {
     typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
     const int half = lane >> 5, grp = (lane >> 4) & 1, s16 = lane & 15, r = half * 4 + (s16 >> 2);
     const uint32_t at = (uint32_t)(r * kRow + ((v_turn(r) << 4) ^ (grp * 32 + (s16 & 3) * 8)));
@@ -40,7 +38,7 @@ struct BfTile {
         const uint8_t* from = tile + (at ^ (uint32_t)(e * 64)) + st * 16 * kRow;
         const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)from);
         const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(from + 8 * kRow));
-        f.av[st][e] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        f[st * NE + e] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
   }
   static __device__ __forceinline__ void logits(const bf16x8 (&a)[NP], const bf16x8 (&qf)[NP], f32x16& s) {
@@ -49,12 +47,12 @@ struct BfTile {
 #pragma unroll
     for (int i = 0; i < NP; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], qf[i], s, 0, 0, 0);
   }
-  static __device__ __forceinline__ void pv(const Frags& f, const bf16x8 (&pb)[2], f32x16 (&acc)[NE]) {
+  static __device__ __forceinline__ void pv(const i16x8 (&f)[2 * NE], const bf16x8 (&pb)[2], f32x16 (&acc)[NE]) {
 #pragma unroll
     for (int st = 0; st < 2; ++st)
 #pragma unroll
       for (int e = 0; e < NE; ++e)
-        acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f.av[st][e]), pb[st], acc[e], 0, 0, 0);
+        acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[st * NE + e]), pb[st], acc[e], 0, 0, 0);
   }
 };
 
@@ -62,18 +60,14 @@ struct BfTile {
 __device__ __forceinline__ void mask_logits(f32x16& s, uint32_t seen, int half) {
   seen >>= 4 * half;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s[i] = seen >> (8 * (i >> 2) + (i & 3)) & 1 ? s[i] : -INFINITY;
+  for (int i = 0; i < 16; ++i) s[i] = or_minus_infinity(s[i], bit_mask(seen, 8 * (i >> 2) + (i & 3)));
 }
 
 // Softmax numerators of a tile's raw logits as the B operands of the second product, against a reference that moves when a maximum exceeds it by
 // more than kRescaleSlack (attn_tile_math.h).  Rounded to bf16, the type of what they multiply: half a step, 2^-8, of each numerator,
 // as much as the rounding of the result.
 template <int NE>
-__device__ __forceinline__ void numerators(f32x16& s, float scale_log2, float& m_ref, float& l_run, f32x16 (&acc)[NE], bf16x8 (&pb)[2]) {
-  float m_loc = s[0];
-#pragma unroll
-  for (int i = 1; i < 16; ++i) m_loc = fmaxf(m_loc, s[i]);
-  m_loc *= scale_log2;
+__device__ __forceinline__ void move_reference_to(float m_loc, float& m_ref, float& l_run, f32x16 (&acc)[NE]) {
   if (__ballot(m_loc > m_ref + kRescaleSlack) != 0) {
     const float m_new = fmaxf(m_ref, fmaxf(m_loc, __shfl_xor(m_loc, 32)));
     const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
@@ -84,6 +78,14 @@ __device__ __forceinline__ void numerators(f32x16& s, float scale_log2, float& m
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[e][i] *= alpha;
   }
+}
+
+template <int NE>
+__device__ __forceinline__ void numerators(const f32x16& s, float scale_log2, float& m_ref, float& l_run, f32x16 (&acc)[NE], bf16x8 (&pb)[2]) {
+  float m_loc = s[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) m_loc = fmaxf(m_loc, s[i]);
+  move_reference_to<NE>(m_loc * scale_log2, m_ref, l_run, acc);
   float l_loc = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
@@ -94,73 +96,83 @@ __device__ __forceinline__ void numerators(f32x16& s, float scale_log2, float& m
   l_run += l_loc;
 }
 
-// A masked tile's values that are no numbers (paged_tile.h): taken out of the operands, and what they make of the results added
-template <int HD>
-__device__ __forceinline__ void split_off_specials(typename BfTile<HD>::Frags& f, uint32_t seen, int half, f32x16 (&acc)[BfTile<HD>::NE]) {
-  constexpr int NE = BfTile<HD>::NE;
-  bool any = false;
+// Takes values that are no numbers out of a masked tile's operands (paged_tile.h), two values a word; true for all lanes if there are any.
+template <int N>
+__device__ __forceinline__ bool take_specials(i16x8 (&f)[N]) {
+  // bits 15 and 31: the exponents that are all ones
+  auto special = [](uint32_t v) { return ((v & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };
+  uint32_t any = 0;
 #pragma unroll
-  for (int st = 0; st < 2; ++st)
+  for (int i = 0; i < N; ++i) {
+    const u32x4 v = __builtin_bit_cast(u32x4, f[i]);
 #pragma unroll
-    for (int e = 0; e < NE; ++e)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) any |= (f.av[st][e][j] & 0x7f80) == 0x7f80;
-  if (__ballot(any) == 0) return;
-  seen >>= 4 * half;
-  bf16x8 one[2];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) one[i >> 3][i & 7] = (__bf16)(seen >> (8 * (i >> 2) + (i & 3)) & 1 ? 1.f : 0.f);
-#pragma unroll
-  for (int e = 0; e < NE; ++e) {
-    f32x16 sums;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sums[i] = 0.f;
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      bf16x8 codes;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const short v = f.av[st][e][j];
-        const bool special = (v & 0x7f80) == 0x7f80;
-        codes[j] = (__bf16)(special ? special_code((float)__builtin_bit_cast(__bf16, v)) : 0.f);
-        f.av[st][e][j] = special ? (short)0 : v;
-      }
-      sums = __builtin_amdgcn_mfma_f32_32x32x16_bf16(codes, one[st], sums, 0, 0, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[e][i] += special_sum(sums[i]);
+    for (int j = 0; j < 4; ++j) any |= special(v[j]);
   }
+  if (__ballot(any != 0) == 0) return false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    u32x4 v = __builtin_bit_cast(u32x4, f[i]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] &= ~((special(v[j]) >> 15) * 0xffffu);
+    f[i] = __builtin_bit_cast(i16x8, v);
+  }
+  return true;
 }
 
-// Where the rows of a tile are (bf16): rows 0-15 and 16-31 lie in one page each, or in the same.  Wave-uniform.
-struct TileBase { const char *k[2], *v[2]; uint32_t stride; int lo, hi; };
+// add_specials' share of one row of V
+template <int NE>
+__device__ __forceinline__ void add_special_row(const char* v, bool sees, int half, f32x16 (&acc)[NE]) {
+#pragma unroll
+  for (int e = 0; e < NE; ++e)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const bf16x4 u = *reinterpret_cast<const bf16x4*>(v + 2 * out_col0(e, i4, half));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[e][i4 * 4 + k] += sees && !(fabsf((float)u[k]) < INFINITY) ? (float)u[k] : 0.f;
+    }
+}
+
+// Where the rows of an item are (bf16), in bytes: its pages' and its own (kSeeTree) rows of the KV head
+struct ItemBase {
+  const char *k, *v, *k_own, *v_own;
+  int64_t page;
+  uint32_t stride, stride_own, row_mask;
+};
+template <int SEES>
+__device__ __forceinline__ ItemBase item_base(const PagedAttnParams& p, const PagedItem& w) {
+  ItemBase r{};
+  const PagedCache& c = p.cache;
+  const int64_t at = 2 * (w.g * c.sh);
+  r.k = (const char*)p.k_pages + at;
+  r.v = (const char*)p.v_pages + at;
+  r.page = 2 * c.sp;
+  r.stride = (uint32_t)(c.sr * 2);
+  r.row_mask = (1u << c.page_shift) - 1;
+  if (SEES == kSeeTree) {
+    const int64_t own = 2 * (w.b * p.blk_sb + w.g * p.blk_sh);
+    r.k_own = (const char*)p.k_blk + own;
+    r.v_own = (const char*)p.v_blk + own;
+    r.stride_own = (uint32_t)(p.blk_sr * 2);
+  }
+  return r;
+}
+
+// Where the rows of a tile are: rows 0-15 and 16-31 lie in one page each, or in the same.  Wave-uniform.
+struct TileBase { int64_t at[2]; uint32_t stride; int lo, hi; bool own; };
 
 // page[h]: page of the first row in half h that somebody sees
 template <int SEES>
-__device__ __forceinline__ TileBase tile_base(const PagedAttnParams& p, const PagedItem& w, const PagedTile& x, const int (&page)[2]) {
+__device__ __forceinline__ TileBase tile_base(const ItemBase& i, const PagedTile& x, const int (&page)[2]) {
   TileBase r;
   r.lo = x.lo;
   r.hi = x.hi;
-  if (SEES == kSeeTree && x.own) {
-    r.stride = (uint32_t)(p.blk_sr * 2);
-    const int64_t at = 2 * (w.b * p.blk_sb + w.g * p.blk_sh + x.at * p.blk_sr);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      // rows of the second half that are not there are copies of the first's last
-      const int64_t half = h == 1 && x.hi > 16 ? 16 * (int64_t)r.stride : 0;
-      r.k[h] = (const char*)p.k_blk + at + half;
-      r.v[h] = (const char*)p.v_blk + at + half;
-    }
-    return r;
-  }
-  const PagedCache& c = p.cache;
-  r.stride = (uint32_t)(c.sr * 2);
+  r.own = SEES == kSeeTree && x.own;
+  r.stride = r.own ? i.stride_own : i.stride;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
+    // a half that nobody sees any of is the other's rows
     const int first = (x.at + min(max(16 * h, x.lo), x.hi - 1)) & ~15;
-    const int64_t at = 2 * (page[h] * c.sp + w.g * c.sh + (first & ((1 << c.page_shift) - 1)) * c.sr);
-    r.k[h] = (const char*)p.k_pages + at;
-    r.v[h] = (const char*)p.v_pages + at;
+    r.at[h] = r.own ? (int64_t)first * i.stride_own : page[h] * i.page + (int64_t)(first & (int)i.row_mask) * i.stride;
   }
   return r;
 }

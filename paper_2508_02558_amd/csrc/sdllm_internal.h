@@ -354,6 +354,7 @@ hipError_t launch_append_paged(const AppendParams& p, int dtype, int d, hipStrea
 struct PagedPlan { int kernel, block_cols, waves, max_blocks, workgroups, least_tiles; bool splits; };
 hipError_t launch_attn_paged(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
 hipError_t launch_attn_paged_f32(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
+hipError_t launch_attn_paged_shared(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
 hipError_t launch_attn_paged_stream(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
 
 }  // namespace sdllm
