@@ -119,56 +119,57 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
 #pragma unroll
       for (int i = 0; i < NP; ++i) qf[i] = __builtin_bit_cast(bf16x8, q[i * 2 + half]);
     }
-    // pages of tiles 64 i .. 64 i + 63 of the share, one per lane
-    int pages[2] = {0, 0};
-    auto look_up = [&](int n0) __attribute__((always_inline)) {
-      const int t = t0 + min(n0 + lane, n_tiles - 1);
-      const PagedTile x = tile_of<SEES>(p, w, t);
-      if (SEES == kSeeTree && x.own) return;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) pages[h] = (int)page_of(p.cache, w.b, x.at + min(max(16 * h, x.lo), x.hi - 1));
-    };
-    // A step's fetch: wave w brings rows w, w + 8, ... of every group's tiles.  A tile past the last is the last one again, masked later.  `from` of K
-    // serves V, which is asked for an iteration later.
-    const uint32_t lds0 = lds_address(smem);
-    // What a lane's place in a fetch is made of is made again every time: there are no registers to keep it in
-    struct Lane { int row, half; bool second; uint32_t k_piece, v_piece; };   // second: of the two tiles of a step (head_dim 64)
-    auto lane_of = [&]() __attribute__((always_inline)) {
-      int l = lane;
-      asm volatile("" : "+v"(l));
-      const int r = S::fetch_row(wave, l);
-      return Lane{r & (kTileKeys - 1), (r >> 4) & 1, r >= kTileKeys, S::fetch_k_piece(l), S::fetch_v_piece(l)};
-    };
+    // Tiles 64 i .. 64 i + 63 of the share, one per lane: where they are, and which of them and of the 64 before every row of this wave sees whole
     const ItemBase item = item_base<SEES>(p, w);
-    struct From { int64_t at; bool own; };
-    auto locate = [&](const Lane& me, int n) __attribute__((always_inline)) {                            // tile n of the share: this lane's half of it
-      n = min(n, n_tiles - 1);
-      const PagedTile x = tile_of<SEES>(p, w, t0 + n);
-      const int page[2] = {__builtin_amdgcn_readlane(pages[0], n & 63), __builtin_amdgcn_readlane(pages[1], n & 63)};
-      const TileBase b = tile_base<SEES>(item, x, page);
-      return From{(me.half ? b.at[1] : b.at[0]) + row_in_half(b, me.row) * b.stride, b.own};
+    TilePlace places;
+    uint64_t whole_now = 0, whole_before = 0;
+    int at_hand = 0;
+    auto look_up = [&](int n0) __attribute__((always_inline)) {
+      const PagedTile x = tile_of<SEES>(p, w, t0 + min(n0 + lane, n_tiles - 1));
+      places = place_of<SEES>(p, w, item, x);
+      whole_before = whole_now;
+      whole_now = __ballot(x.full && n0 + lane < n_tiles);
+      at_hand = n0 >> 6;
     };
-    From from[KS];
-    auto fetch_k = [&](int step, int slot) __attribute__((always_inline)) {
-      const Lane me = lane_of();
+    // A step's fetch: wave w brings rows w, w + 8, ... of every group's tiles.  A tile past the last is the last one again, masked later.
+    const uint32_t lds0 = lds_address(smem);
+    const int my_row = S::fetch_row(wave, lane);
+    const uint32_t off_k = (uint32_t)(my_row & (kTileKeys - 1)) * item.stride + S::fetch_k_piece(lane);
+    const uint32_t off_v = (uint32_t)(my_row & (kTileKeys - 1)) * item.stride + S::fetch_v_piece(lane);
+    auto fetch = [&](bool is_v, int step, int slot) __attribute__((always_inline)) {
+      const char *pages = is_v ? item.v : item.k, *own = is_v ? item.v_own : item.k_own;
+      const uint32_t off = is_v ? off_v : off_k;
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
-        const int n = (step * KS + i) * KT;
-        if constexpr (KT == 1) {
-          from[i] = locate(me, n);
+        const uint32_t to = lds0 + (uint32_t)(slot + (is_v ? kV0 + i * kRingV + wave * kVGroup : i * kRingK + wave * kKGroup));
+        const int n = (step * KS + i) * KT, n0 = min(n, n_tiles - 1) & 63, n1 = min(n + KT - 1, n_tiles - 1) & 63;
+        const uint32_t bits0 = (uint32_t)__builtin_amdgcn_readlane((int)places.bits, n0), bits1 = (uint32_t)__builtin_amdgcn_readlane((int)places.bits, n1);
+        if (bits0 & bits1 & kWhole) {
+          const int64_t a = readlane64(places.at0, n0);
+          if constexpr (KT == 1) {
+            fetch_to_lds(to, pages + a, off);
+          } else {
+            const int64_t b = readlane64(places.at0, n1);
+            fetch_to_lds(to, pages + (my_row >= kTileKeys ? b : a) + off);
+          }
         } else {
-          const From a = locate(me, n), b = locate(me, n + 1);
-          from[i] = From{me.second ? b.at : a.at, me.second ? b.own : a.own};
+          int l = lane;
+          asm volatile("" : "+v"(l));   // worked out here, not kept
+          const int row = S::fetch_row(wave, l);
+          const TilePlace a = place_from(places, n0);
+          const char* from = (a.bits & kOwn ? own : pages) + row_at(a, item, row & (kTileKeys - 1));
+          if constexpr (KT > 1) {
+            const TilePlace b = place_from(places, n1);
+            const char* other = (b.bits & kOwn ? own : pages) + row_at(b, item, row & (kTileKeys - 1));
+            from = row >= kTileKeys ? other : from;
+          }
+          fetch_to_lds(to, from + (is_v ? S::fetch_v_piece(l) : S::fetch_k_piece(l)));
         }
-        fetch_to_lds(lds0 + (uint32_t)(slot + i * kRingK + wave * kKGroup), (from[i].own ? item.k_own : item.k) + from[i].at + me.k_piece);
       }
     };
-    auto fetch_v = [&](int slot) __attribute__((always_inline)) {                        // of the step whose K was asked for last
-      const Lane me = lane_of();
-#pragma unroll
-      for (int i = 0; i < KS; ++i) fetch_to_lds(lds0 + (uint32_t)(kV0 + slot + i * kRingV + wave * kVGroup), (from[i].own ? item.v_own : item.v) + from[i].at + me.v_piece);
-    };
-    // the 64 tiles whose pages are at hand change before a step that begins with the next
+    auto fetch_k = [&](int step, int slot) __attribute__((always_inline)) { fetch(false, step, slot); };
+    auto fetch_v = [&](int step, int slot) __attribute__((always_inline)) { fetch(true, step, slot); };
+    // The 64 tiles at hand change before the K of a step that begins with the next; V of the step before has been asked for by then.
     auto turn_page = [&](int step) __attribute__((always_inline)) {
       const int n = step * KS * KT;
       if ((n & 63) == 0 && n < n_tiles) look_up(n);
@@ -183,15 +184,14 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
 
     bool full;
     auto mask = [&](int step) __attribute__((always_inline)) {
-      full = true;
+      const int n0 = (step * KS + kg) * KT;
+      const uint64_t whole = (n0 >> 6 == at_hand ? whole_now : whole_before) >> (n0 & 63);
+      full = (~whole & ((1u << KT) - 1)) == 0;
+      if (full) return;
 #pragma unroll
       for (int q = 0; q < KT; ++q) {
-        const int n = (step * KS + kg) * KT + q;
-        const PagedTile x = tile_of<SEES>(p, w, t0 + min(n, n_tiles - 1));
-        if (n >= n_tiles || !x.full) {
-          full = false;
-          mask_logits(sn[q], n >= n_tiles ? 0u : seen_bits<SEES>(p, x, sight), half);
-        }
+        const PagedTile x = tile_of<SEES>(p, w, t0 + min(n0 + q, n_tiles - 1));
+        mask_logits(sn[q], n0 + q >= n_tiles ? 0u : seen_bits<SEES>(p, x, sight), half);
       }
     };
     // Vector phase of a step: masks, row maxima, the reference, first half of the numerators
@@ -244,7 +244,7 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
     // (pages, masks, query rows) make a wait longer, never shorter.
     look_up(0);
     fetch_k(0, 0);
-    fetch_v(0);
+    fetch_v(0, 0);
     turn_page(1);
     fetch_k(1, kStepK);
     in_issue_order();
@@ -258,7 +258,7 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
         turn_page(j);
         fetch_k(j, j * kStepK);
       }
-      fetch_v(j * kStepV);
+      fetch_v(j, j * kStepV);
     }
     in_issue_order();
 #pragma unroll
@@ -298,7 +298,7 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
       __builtin_amdgcn_s_setprio(0);
       bare_barrier();
       if (fetches) {
-        fetch_v(v_next);
+        fetch_v(t + N, v_next);
         turn_page(t + N + 1);
         fetch_k(t + N + 1, k_next);
       }

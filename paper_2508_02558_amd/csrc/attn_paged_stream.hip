@@ -38,32 +38,30 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   const RowSight sight = sight_of<SEES>(p, w, row);
 
   const ItemBase item = item_base<SEES>(p, w);
-  // pages of tiles 64 i .. 64 i + 63 of this wavefront's, one per lane
-  int pages[2] = {0, 0};
+  // tiles 64 i .. 64 i + 63 of this wavefront's, one per lane: where they are
+  TilePlace places;
   auto look_up = [&](int j0) __attribute__((always_inline)) {
-    const int t = min(t_begin + (j0 + lane) * nw, w.tiles - 1);
-    const PagedTile x = tile_of<SEES>(p, w, t);
-    if (SEES == kSeeTree && x.own) return;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) pages[h] = (int)page_of(p.cache, w.b, x.at + min(max(16 * h, x.lo), x.hi - 1));
-  };
-  auto base_of = [&](int j, PagedTile& x) __attribute__((always_inline)) {
-    x = tile_of<SEES>(p, w, t_begin + j * nw);
-    const int page[2] = {__builtin_amdgcn_readlane(pages[0], j & 63), __builtin_amdgcn_readlane(pages[1], j & 63)};
-    return tile_base<SEES>(item, x, page);
+    places = place_of<SEES>(p, w, item, tile_of<SEES>(p, w, min(t_begin + (j0 + lane) * nw, w.tiles - 1)));
   };
 
   uint8_t* k_lds = smem + wave * kWaveLds;
   uint8_t* v_lds = k_lds + T::kBytes;
   const int r0 = lane / T::kPieces, place = lane % T::kPieces;
-  auto fetch = [&](const TileBase& t, bool is_v, uint8_t* lds) __attribute__((always_inline)) {
-    const uint32_t to = lds_address(lds);
+  auto fetch = [&](const TilePlace& t, bool is_v, uint8_t* lds) __attribute__((always_inline)) {
+    const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_address(lds));
+    const char* base = t.bits & kOwn ? is_v ? item.v_own : item.k_own : is_v ? item.v : item.k;
+    auto piece = [&](int r) __attribute__((always_inline)) { return (uint32_t)(place ^ (is_v ? T::v_turn(r) : T::k_turn(r))) << 4; };
+    if (t.bits & kWhole) {
 #pragma unroll
-    for (int j = 0; j < T::kFetches; ++j) {
-      const int r = j * T::kRowsPerFetch + r0, h = j * T::kRowsPerFetch >> 4;
-      const char* base = (t.own ? is_v ? item.v_own : item.k_own : is_v ? item.v : item.k) + t.at[h];
-      const uint32_t piece = (uint32_t)(place ^ (is_v ? T::v_turn(r) : T::k_turn(r))) << 4;
-      fetch_to_lds(to + (uint32_t)j * 1024, in_scalars(base), row_in_half(t, r) * t.stride + piece);
+      for (int j = 0; j < T::kFetches; ++j)
+        fetch_to_lds_once(to + (uint32_t)j * 1024, in_scalars(base + t.at0 + (int64_t)(j * T::kRowsPerFetch) * item.stride),
+                     r0 * item.stride + piece(j * T::kRowsPerFetch + r0));
+    } else {
+#pragma unroll
+      for (int j = 0; j < T::kFetches; ++j) {
+        const int r = j * T::kRowsPerFetch + r0;
+        fetch_to_lds_once(to + (uint32_t)j * 1024, base + row_at(t, item, r) + piece(r));
+      }
     }
   };
 
@@ -80,7 +78,7 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   // Requests in order: K(0), V(0), K(1), and then for each tile j K(j+2), V(j+1).  The waits count them.  Loads by the compiler in between (pages)
   // make a wait longer, never shorter.
   PagedTile x, x_next;
-  TileBase base_next;
+  TilePlace next;
   auto landed = [&](bool all) __attribute__((always_inline)) {
     if (all) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     else if constexpr (T::kFetches == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
@@ -95,8 +93,9 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (j + 1 < n_mine) {
       if (((j + 1) & 63) == 0) look_up(j + 1);
-      base_next = base_of(j + 1, x_next);
-      fetch(base_next, false, k_lds);
+      next = place_from(places, (j + 1) & 63);
+      x_next = tile_of<SEES>(p, w, t_begin + (j + 1) * nw);
+      fetch(next, false, k_lds);
     }
     in_issue_order();
     T::logits(a, qf, s);
@@ -108,18 +107,20 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   };
   if (n_mine > 0) {
     look_up(0);
-    TileBase base_v = base_of(0, x_next);
-    fetch(base_v, false, k_lds);
+    x_next = tile_of<SEES>(p, w, t_begin);
+    TilePlace of_v = place_from(places, 0);
+    fetch(of_v, false, k_lds);
     in_issue_order();
-    fetch(base_v, true, v_lds);
+    fetch(of_v, true, v_lds);
     in_issue_order();
     const u32x4* q = reinterpret_cast<const u32x4*>((const char*)p.q + 2 * (w.b * p.q_sb + head * p.q_sh + row * p.q_sr));
 #pragma unroll
     for (int i = 0; i < T::NP; ++i) qf[i] = __builtin_bit_cast(bf16x8, q[i * 2 + half]);
     // logits of tile j, second product of tile j - 1, softmax of tile j
+#pragma clang loop unroll(disable)
     for (int j = 0; j <= n_mine; ++j) {
       if (j < n_mine) {
-        if (j > 0) base_v = base_next;
+        if (j > 0) of_v = next;
         landed(j <= 1);                     // K(j); V(j-1) may still fly
         logits(j);
       }
@@ -127,7 +128,7 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
         landed(j + 1 >= n_mine);            // V(j-1); K(j+1), if there is one, may still fly
         T::read_v(v_lds, lane, f);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (j < n_mine) fetch(base_v, true, v_lds);
+        if (j < n_mine) fetch(of_v, true, v_lds);
         in_issue_order();
         if (!full) specials |= take_specials(f);
         T::pv(f, pb, acc);

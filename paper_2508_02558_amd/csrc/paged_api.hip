@@ -124,6 +124,8 @@ int32_t run_paged(const sdllm_paged_shape_t* shape, bool tree, const void* q, co
     p.part_ml = (float*)((char*)ws + bytes.part_o);
     p.item_at = (int32_t*)((char*)ws + bytes.part_o + bytes.part_ml);
   }
+  p.chunk = std::min(pl.max_blocks, 4);
+  p.by_chunk = Divisor((uint32_t)p.chunk);
   p.by_group = Divisor((uint32_t)p.group); p.by_blocks = Divisor((uint32_t)p.max_blocks); p.by_hkv = Divisor((uint32_t)p.hkv);
   return launch_attn_paged(p, pl, tree ? kSeeTree : kSeeWindow, s.head_dim, (hipStream_t)stream) == hipSuccess ? SDLLM_OK : SDLLM_ERR_HIP;
 }

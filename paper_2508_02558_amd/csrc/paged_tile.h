@@ -23,6 +23,15 @@ struct PagedItem {
   int first_tile, tiles;    // first tile of the window; tiles in all
 };
 
+// Workgroup ids are dealt round-robin over the XCDs, and by each XCD over its shader engines, without regard to how long a workgroup takes.  So is the
+// work: every XCD takes `chunk` neighbours, which read the same keys, of every 8 chunk ids, and every other turn goes backwards over XCDs and neighbours,
+// so that ids in descending order of work come out even.  (Contiguous ranges, xcd_contiguous_id, give an XCD whole sequences.)
+__device__ __forceinline__ int chunked_id(const PagedAttnParams& p, int dealt, int n) {
+  const int x = dealt % kNumXCDs, s = dealt / kNumXCDs, turn = p.by_chunk.quotient(s), e = s - turn * p.chunk;
+  if (dealt >= p.by_chunk.quotient(n / kNumXCDs) * p.chunk * kNumXCDs) return dealt;
+  return turn & 1 ? (turn * kNumXCDs + kNumXCDs - 1 - x) * p.chunk + p.chunk - 1 - e : (turn * kNumXCDs + x) * p.chunk + e;
+}
+
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 template <int SEES>
@@ -76,13 +85,14 @@ template <int SEES>
 __device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, PagedItem& w) {
   if (!p.part_o) {
     // Items as workgroups, the last block of a head first: with all past keys to see it has the most tiles
-    const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
-    const int head = p.by_blocks.quotient(id);
-    w.blk = p.max_blocks - 1 - (id - head * p.max_blocks);
+    const int id = chunked_id(p, blockIdx.x, gridDim.x);
+    const int head = p.by_blocks.quotient(id), rank = id - head * p.max_blocks;
     w.b = p.by_hkv.quotient(head);
     w.g = head - w.b * p.hkv;
     w.count = __builtin_amdgcn_readfirstlane(p.cache.count(w.b));
-    if (w.blk * p.block_cols >= w.count * p.group) return false;
+    const int blocks = blocks_of(p, w.count);
+    if (rank >= blocks) return false;
+    w.blk = blocks - 1 - rank;
     w.length = __builtin_amdgcn_readfirstlane(p.cache.length(w.b));
     w.split = 0;
     w.n_split = 1;
@@ -121,7 +131,7 @@ __device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, Pa
   }
   used = __builtin_amdgcn_readfirstlane(sum(used));
   if ((int)blockIdx.x >= used) return false;
-  const int id = xcd_contiguous_id(blockIdx.x, used);
+  const int id = chunked_id(p, blockIdx.x, used);
   int before = 0;
   for (int b0 = 0; b0 < p.batch; b0 += kWave) {
     const Seq s = sequence_at(b0);

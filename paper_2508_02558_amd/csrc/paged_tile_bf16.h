@@ -157,27 +157,39 @@ __device__ __forceinline__ ItemBase item_base(const PagedAttnParams& p, const Pa
   return r;
 }
 
-// Where the rows of a tile are: rows 0-15 and 16-31 lie in one page each, or in the same.  Wave-uniform.
-struct TileBase { int64_t at[2]; uint32_t stride; int lo, hi; bool own; };
+// Where the rows of a tile are, worked out for 64 tiles at once, one per lane, and handed out by readlane.  Rows 0-15 and 16-31 lie in one page each, or in the
+// same; a half that nobody sees any of is the other's rows.
+struct TilePlace {
+  int64_t at0, at1; // bytes from ItemBase's pointers to row 0 and to row 16
+  uint32_t bits;    // of [lo, hi): lo, hi << 6; kOwn, kWhole
+};
+constexpr uint32_t kOwn = 1 << 12, kWhole = 1 << 13;   // kWhole: 32 rows of the cache, one stride apart
 
-// page[h]: page of the first row in half h that somebody sees
 template <int SEES>
-__device__ __forceinline__ TileBase tile_base(const ItemBase& i, const PagedTile& x, const int (&page)[2]) {
-  TileBase r;
-  r.lo = x.lo;
-  r.hi = x.hi;
-  r.own = SEES == kSeeTree && x.own;
-  r.stride = r.own ? i.stride_own : i.stride;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    // a half that nobody sees any of is the other's rows
-    const int first = (x.at + min(max(16 * h, x.lo), x.hi - 1)) & ~15;
-    r.at[h] = r.own ? (int64_t)first * i.stride_own : page[h] * i.page + (int64_t)(first & (int)i.row_mask) * i.stride;
-  }
+__device__ __forceinline__ TilePlace place_of(const PagedAttnParams& p, const PagedItem& w, const ItemBase& i, const PagedTile& x) {
+  TilePlace r;
+  const bool own = SEES == kSeeTree && x.own;
+  auto half_at = [&](int h) {
+    const int seen = x.at + min(max(16 * h, x.lo), x.hi - 1), first = seen & ~15;
+    return own ? (int64_t)first * i.stride_own : page_of(p.cache, w.b, seen) * i.page + (int64_t)(first & (int)i.row_mask) * i.stride;
+  };
+  r.at0 = half_at(0);
+  r.at1 = half_at(1);
+  const bool whole = !own && x.lo == 0 && x.hi == kTileKeys && r.at1 - r.at0 == 16 * (int64_t)i.stride;
+  r.bits = (uint32_t)(x.lo | x.hi << 6) | (own ? kOwn : 0u) | (whole ? kWhole : 0u);
   return r;
 }
-
-// Row of a half's page that stands at row r of the tile: itself, or the nearest that somebody sees
-__device__ __forceinline__ uint32_t row_in_half(const TileBase& t, int r) { return (uint32_t)(min(max(r, t.lo), t.hi - 1) & 15); }
+__device__ __forceinline__ int64_t readlane64(int64_t v, int lane) {
+  const uint64_t u = (uint64_t)v;
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)u, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), lane) << 32);
+}
+__device__ __forceinline__ TilePlace place_from(const TilePlace& r, int lane) {
+  return {readlane64(r.at0, lane), readlane64(r.at1, lane), (uint32_t)__builtin_amdgcn_readlane((int)r.bits, lane)};
+}
+// Row r of a tile, or the nearest that somebody sees, in bytes from ItemBase's pointers
+__device__ __forceinline__ int64_t row_at(const TilePlace& t, const ItemBase& i, int r) {
+  r = min(max(r, (int)(t.bits & 63)), (int)(t.bits >> 6 & 63) - 1);
+  return t.at0 + ((r & 16) != 0 ? t.at1 - t.at0 : 0) + (uint32_t)(r & 15) * (t.bits & kOwn ? i.stride_own : i.stride);
+}
 
 }  // namespace sdllm

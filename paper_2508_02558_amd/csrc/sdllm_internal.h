@@ -340,7 +340,8 @@ struct PagedAttnParams {
   float* part_o;                      // [workgroups][block_cols][d]; null: nothing is split, workgroups are the items
   float* part_ml;                     // [workgroups][2][block_cols]
   int32_t* item_at;                   // [batch x hkv x max_blocks][2]: first of an item's workgroups in part_*, how many
-  Divisor by_group, by_blocks, by_hkv;
+  int32_t chunk;                      // neighbours among the workgroups that go to one XCD
+  Divisor by_group, by_blocks, by_hkv, by_chunk;
 };
 
 // Most wavefronts of a workgroup: with fp32 tensors the three parts of the queries take the registers of two
