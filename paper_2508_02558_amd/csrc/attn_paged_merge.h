@@ -18,11 +18,10 @@ __global__ __launch_bounds__(kPagedMergeThreads) void attn_paged_merge_kernel(co
   const int col = tid / kPer, sub = tid % TPI, c4 = tid % kPer / TPI * 4;
   const int head = p.by_blocks.quotient(item), blk = item - head * p.max_blocks;
   const int b = p.by_hkv.quotient(head), g = head - b * p.hkv;
-  // an item that is not there has left nothing, not even its place
   const int column = blk * p.block_cols + col;
-  if (column >= p.cache.count(b) * p.group || col >= p.block_cols) return;
   const int slot = p.item_at[2 * item], n_split = p.item_at[2 * item + 1];
-  if (n_split < 2) return;
+  // an item that is not there has left nothing, not even its place
+  if (column >= p.cache.count(b) * p.group || col >= p.block_cols || n_split < 2) return;
   const float* ml = p.part_ml + (int64_t)slot * 2 * p.block_cols + col;
   const float* po = p.part_o + ((int64_t)slot * p.block_cols + col) * D + c4;
   RowPiece r;

@@ -11,7 +11,7 @@ namespace sdllm {
 
 namespace {
 
-constexpr int kStreamWaves = 4;   // most of a workgroup; two workgroups share a CU
+constexpr int kStreamWaves = 8;   // most of a workgroup
 
 template <int HD>
 constexpr int stream_wave_lds() { return 2 * BfTile<HD>::kBytes + 256; }   // K, V and row statistics; the accumulators are parked where the tiles were
@@ -46,21 +46,30 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
 
   uint8_t* k_lds = smem + wave * kWaveLds;
   uint8_t* v_lds = k_lds + T::kBytes;
-  const int r0 = lane / T::kPieces, place = lane % T::kPieces;
-  auto fetch = [&](const TilePlace& t, bool is_v, uint8_t* lds) __attribute__((always_inline)) {
+  const bool past_caches = w.past_caches;
+  auto fetch = [&](TilePlace t, bool is_v, uint8_t* lds) __attribute__((always_inline)) {
     const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_address(lds));
     const char* base = t.bits & kOwn ? is_v ? item.v_own : item.k_own : is_v ? item.v : item.k;
+    int l = lane;
+    asm volatile("" : "+v"(l));   // a lane's places in the fetches are worked out here: kept, they would be too many registers
+    const int r0 = l / T::kPieces, place = l % T::kPieces;
     auto piece = [&](int r) __attribute__((always_inline)) { return (uint32_t)(place ^ (is_v ? T::v_turn(r) : T::k_turn(r))) << 4; };
     if (t.bits & kWhole) {
+      const uint32_t off = r0 * item.stride;
+      const char* first = base + t.at0;
+      const int64_t step = (int64_t)T::kRowsPerFetch * item.stride;
+      if (past_caches) {
 #pragma unroll
-      for (int j = 0; j < T::kFetches; ++j)
-        fetch_to_lds_once(to + (uint32_t)j * 1024, in_scalars(base + t.at0 + (int64_t)(j * T::kRowsPerFetch) * item.stride),
-                     r0 * item.stride + piece(j * T::kRowsPerFetch + r0));
+        for (int j = 0; j < T::kFetches; ++j) fetch_to_lds_once(to + (uint32_t)j * 1024, in_scalars(first + j * step), off + piece(j * T::kRowsPerFetch + r0));
+      } else {
+#pragma unroll
+        for (int j = 0; j < T::kFetches; ++j) fetch_to_lds(to + (uint32_t)j * 1024, in_scalars(first + j * step), off + piece(j * T::kRowsPerFetch + r0));
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < T::kFetches; ++j) {
         const int r = j * T::kRowsPerFetch + r0;
-        fetch_to_lds_once(to + (uint32_t)j * 1024, base + row_at(t, item, r) + piece(r));
+        fetch_to_lds(to + (uint32_t)j * 1024, base + row_at(t, item, r) + piece(r));
       }
     }
   };
@@ -78,7 +87,7 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   // Requests in order: K(0), V(0), K(1), and then for each tile j K(j+2), V(j+1).  The waits count them.  Loads by the compiler in between (pages)
   // make a wait longer, never shorter.
   PagedTile x, x_next;
-  TilePlace next;
+  TilePlace next{};
   auto landed = [&](bool all) __attribute__((always_inline)) {
     if (all) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     else if constexpr (T::kFetches == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
@@ -120,7 +129,7 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
 #pragma clang loop unroll(disable)
     for (int j = 0; j <= n_mine; ++j) {
       if (j < n_mine) {
-        if (j > 0) of_v = next;
+        if (j > 0) { of_v.at0 = next.at0; of_v.at1 = next.at1; of_v.bits = next.bits; }
         landed(j <= 1);                     // K(j); V(j-1) may still fly
         logits(j);
       }

@@ -54,7 +54,6 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   pl = PagedPlan{};
   pl.kernel = s.dtype == SDLLM_F32 ? kPagedF32 : cols <= 32 ? kPagedStream : kPagedShared;
   pl.block_cols = pl.kernel == kPagedF32 ? kGeneralRowsF32 : pl.kernel == kPagedStream ? 32 : cols <= 128 ? 128 : 256;
-  pl.waves = pl.kernel == kPagedStream ? 4 : kGeneralMaxWaves;
   // columns, blocks and threads of a launch (the merge's too) are counted in 32 bits
   if (cols > INT32_MAX - 256) return SDLLM_ERR_UNSUPPORTED;
   pl.max_blocks = (int)((cols + pl.block_cols - 1) / pl.block_cols);
@@ -68,11 +67,15 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   if (tree) tiles += 2;
   else if (s.window_left >= 0 && s.window_right >= 0)
     tiles = std::min<int64_t>(tiles, ((int64_t)s.window_left + s.window_right + pl.block_cols) / kTileKeys + 2 + std::min(s.sinks, capacity) / kTileKeys);
-  // workgroups that the CUs hold at once
-  const int64_t at_once = pl.kernel == kPagedShared ? kNumCUs : 2 * kNumCUs;
-  pl.least_tiles = pl.kernel == kPagedShared ? 16 : 8;
-  pl.splits = items <= 2 * at_once && tiles > pl.least_tiles;
+  // With few items a workgroup has the eight wavefronts that a CU's LDS has room for, with many of them two of four wavefronts share it, one starting or
+  // merging while the other streams.
+  pl.waves = pl.kernel == kPagedStream && items > 64 ? 4 : 8;
+  const int64_t at_once = pl.waves == 4 ? 2 * kNumCUs : kNumCUs;
+  pl.least_tiles = pl.kernel == kPagedStream ? 6 * pl.waves : 16;
+  // A second round of workgroups that share columns' keys costs more than uneven items do
+  pl.splits = items <= (pl.kernel == kPagedShared ? 160 : 2 * at_once) && tiles > pl.least_tiles;
   pl.workgroups = pl.splits ? (int)std::max<int64_t>(at_once, 2 * items) : (int)items;
+  while (tiles >> pl.tile_shift >= 1 << 20) ++pl.tile_shift;   // items <= 1024
   return SDLLM_OK;
 }
 
@@ -119,11 +122,13 @@ int32_t run_paged(const sdllm_paged_shape_t* shape, bool tree, const void* q, co
   p.sinks = std::min(s.sinks, capacity);
   p.scale_log2 = (s.softmax_scale > 0.f ? s.softmax_scale : 1.0f / sqrtf((float)s.head_dim)) * kLog2e;
   p.block_cols = pl.block_cols; p.max_blocks = pl.max_blocks; p.workgroups = pl.workgroups; p.least_tiles = pl.least_tiles;
+  p.tile_shift = pl.tile_shift;
   if (pl.splits) {
     p.part_o = (float*)ws;
     p.part_ml = (float*)((char*)ws + bytes.part_o);
     p.item_at = (int32_t*)((char*)ws + bytes.part_o + bytes.part_ml);
   }
+  p.caches_tiles = (128 << 20) / (2 * kTileKeys * s.head_dim * elem_size(s.dtype));
   p.chunk = std::min(pl.max_blocks, 4);
   p.by_chunk = Divisor((uint32_t)p.chunk);
   p.by_group = Divisor((uint32_t)p.group); p.by_blocks = Divisor((uint32_t)p.max_blocks); p.by_hkv = Divisor((uint32_t)p.hkv);

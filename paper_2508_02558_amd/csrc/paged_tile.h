@@ -3,8 +3,8 @@
 // The query rows of a KV head are columns: column c is query head c % G of the group and row c / G of the sequence, so that neighbours see nearly the same
 // keys.  A workgroup takes a block of columns (an item) and all 32-key tiles that any of them sees, or a split of those tiles.  Lengths are
 // known on the device only, so every wavefront works out the cut by itself: with W workgroups, n items and N tiles of all items together, a share is
-// c = max(least, ceil(N / (W - n))) tiles and an item with T tiles has ceil(T / c) splits; their sum is below N / c + n <= W.  Two
-// rounds of integer sums over the sequences, 64 of them at a time; nothing is kept between calls.
+// c tiles at most and an item with T tiles has ceil(T / c) splits.  c = ceil(N / (W - n)) is enough for their sum to be W at most, as it is below N / c + n; the
+// least c that is, or near it, is found by halving.  Sums over the sequences, 64 of them at a time; nothing is kept between calls.
 #pragma once
 
 #include "mfma_tile.h"
@@ -19,6 +19,7 @@ struct PagedItem {
   int sink_end;             // first keys that any row of the block sees as such: [0, sink_end)
   int first, last;          // keys of the window of any row: [first, last]
   int least_last, most_first;   // keys [most_first, least_last] are in the window of every row
+  bool past_caches;         // so many tiles are read in all that what is read does not stay in the caches anyway
   int lead_tiles;           // tiles before the window's: of first keys, or (kSeeTree) of the cache
   int first_tile, tiles;    // first tile of the window; tiles in all
 };
@@ -33,6 +34,26 @@ __device__ __forceinline__ int chunked_id(const PagedAttnParams& p, int dealt, i
 }
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+// a / b rounded up, of 0 <= a <= 2^24 + 64 or a ratio below 2^21, and 1 <= b, both below 2^31: the quotient by floats is off by one at most
+__device__ __forceinline__ int ceil_ratio(int a, int b) {
+  int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b));
+  const int64_t r = (int64_t)a - (int64_t)q * b;
+  q += r >= b ? 1 : r < 0 ? -1 : 0;
+  return q + ((int64_t)q * b < a ? 1 : 0);
+}
+
+// Sum of x over the lanes up to this one, in registers (shuffles go through LDS)
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1, 2, 4, 8: within rows of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), kWave - 1); }
 
 template <int SEES>
 __device__ __forceinline__ int last_seen(const PagedAttnParams& p, int end, int place) {
@@ -98,50 +119,50 @@ __device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, Pa
     w.n_split = 1;
     w.slot = 0;
     locate_item<SEES>(p, w);
+    w.past_caches = (int64_t)gridDim.x * w.tiles >= p.caches_tiles;   // a guess: as if all items were like this one
     return true;
   }
-  struct Seq { int blocks, tiles; };
+  struct Seq { int length, count, blocks, tiles; };
   auto sequence = [&](int b) {
-    if (b >= p.batch) return Seq{0, 0};
-    const int count = p.cache.count(b);
-    return Seq{blocks_of(p, count), most_tiles<SEES>(p, p.cache.length(b), count)};
-  };
-  auto sum = [](auto x) {
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) x += __shfl_xor(x, o);
-    return x;
+    if (b >= p.batch) return Seq{0, 0, 0, 0};
+    const int count = p.cache.count(b), length = p.cache.length(b);
+    return Seq{length, count, blocks_of(p, count), most_tiles<SEES>(p, length, count)};
   };
   const Seq mine = sequence(lane);   // the first 64 sequences are looked at once
   auto sequence_at = [&](int b0) { return b0 == 0 ? mine : sequence(b0 + lane); };
-  int items = 0;
-  double tiles = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += kWave) {
-    const Seq s = sequence_at(b0);
-    items += p.hkv * s.blocks;
-    tiles += (double)(p.hkv * s.blocks) * s.tiles;
+  auto over_all = [&](auto f) {
+    int n = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += kWave) {
+      const Seq s = sequence_at(b0);
+      n += f(s, p.hkv * s.blocks);
+    }
+    return wave_sum(n);
+  };
+  const int items = over_all([](const Seq&, int heads) { return heads; });
+  const int tiles = over_all([&](const Seq& s, int heads) { return heads * ((s.tiles >> p.tile_shift) + 1); });   // in units of 2^tile_shift, which add up in 32 bits
+  auto splits_at = [](const Seq& s, int share) { return max(1, ceil_ratio(s.tiles, share)); };
+  auto used_at = [&](int share) { return over_all([&](const Seq& s, int heads) { return heads * splits_at(s, share); }); };
+  // The host launches more workgroups than there can be items: this share is enough, and the least that is lies between N / W and it.
+  int share = (ceil_ratio(tiles, p.workgroups - items) << p.tile_shift) + 1;
+  int used;
+  if (share <= p.least_tiles) {
+    used = used_at(share = p.least_tiles);
+  } else {
+    int too_small = max(p.least_tiles - 1, (tiles / p.workgroups << p.tile_shift) - 1);
+    for (int i = 0; i < 5 && share - too_small > 1; ++i) {
+      const int middle = too_small + (share - too_small) / 2;
+      if (used_at(middle) <= p.workgroups) share = middle;
+      else too_small = middle;
+    }
+    used = used_at(share);
   }
-  items = __builtin_amdgcn_readfirstlane(sum(items));
-  tiles = sum(tiles);
-  // the host launches more workgroups than there can be items
-  const int share = __builtin_amdgcn_readfirstlane(max(p.least_tiles, (int)ceil(tiles / max(1, p.workgroups - items))));
-  int used = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += kWave) {
-    const Seq s = sequence_at(b0);
-    used += p.hkv * s.blocks * max(1, ceil_div(s.tiles, share));
-  }
-  used = __builtin_amdgcn_readfirstlane(sum(used));
   if ((int)blockIdx.x >= used) return false;
+  w.past_caches = (int64_t)tiles << p.tile_shift >= p.caches_tiles;
   const int id = chunked_id(p, blockIdx.x, used);
   int before = 0;
   for (int b0 = 0; b0 < p.batch; b0 += kWave) {
     const Seq s = sequence_at(b0);
-    const int splits = max(1, ceil_div(s.tiles, share)), here = p.hkv * s.blocks * splits;
-    int upto = here;   // of the sequences up to this lane's
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const int x = __shfl_up(upto, o);
-      if (lane >= o) upto += x;
-    }
+    const int splits = splits_at(s, share), here = p.hkv * s.blocks * splits, upto = wave_scan(here);
     const uint64_t past = __ballot(id < before + upto);
     if (past) {
       const int l = __builtin_ctzll(past);
@@ -155,8 +176,8 @@ __device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, Pa
       w.g = unit / w.n_split;
       w.split = unit - w.g * w.n_split;
       w.slot = before + (w.g * blocks + w.blk) * w.n_split + w.split;
-      w.count = __builtin_amdgcn_readfirstlane(p.cache.count(w.b));
-      w.length = __builtin_amdgcn_readfirstlane(p.cache.length(w.b));
+      w.count = __builtin_amdgcn_readlane(s.count, l);
+      w.length = __builtin_amdgcn_readlane(s.length, l);
       locate_item<SEES>(p, w);
       if (w.split == 0 && threadIdx.x == 0) {
         int32_t* at = p.item_at + 2 * ((int64_t)(w.b * p.hkv + w.g) * p.max_blocks + w.blk);

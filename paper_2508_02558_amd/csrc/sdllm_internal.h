@@ -340,6 +340,8 @@ struct PagedAttnParams {
   float* part_o;                      // [workgroups][block_cols][d]; null: nothing is split, workgroups are the items
   float* part_ml;                     // [workgroups][2][block_cols]
   int32_t* item_at;                   // [batch x hkv x max_blocks][2]: first of an item's workgroups in part_*, how many
+  int32_t tile_shift;                 // in units of 2^tile_shift the tiles of all items add up in 32 bits
+  int32_t caches_tiles;               // tiles from which on they are read past the caches
   int32_t chunk;                      // neighbours among the workgroups that go to one XCD
   Divisor by_group, by_blocks, by_hkv, by_chunk;
 };
@@ -352,7 +354,7 @@ hipError_t launch_attn_packed(const PackedAttnParams& p, int dtype, int d, hipSt
 hipError_t launch_qk_norm_rope(const QkParams& p, int dtype, int d, hipStream_t s);
 hipError_t launch_append_paged(const AppendParams& p, int dtype, int d, hipStream_t s);
 // how a call is cut up; pl of a launch or of the host's question
-struct PagedPlan { int kernel, block_cols, waves, max_blocks, workgroups, least_tiles; bool splits; };
+struct PagedPlan { int kernel, block_cols, waves, max_blocks, workgroups, least_tiles, tile_shift; bool splits; };
 hipError_t launch_attn_paged(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
 hipError_t launch_attn_paged_f32(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
 hipError_t launch_attn_paged_shared(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
