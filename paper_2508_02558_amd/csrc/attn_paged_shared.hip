@@ -329,7 +329,14 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
     const int per_step = KS * KT;   // tiles of this group: KT of every step
     add_specials<SEES>(p, w, sight, 2, 0, nsteps * KT,
                        [&](int n) __attribute__((always_inline)) { return t0 + min(n / KT * per_step + kg * KT + n % KT, n_tiles - 1); },
-                       [&](const char* v, bool sees) __attribute__((always_inline)) { add_special_row<NE>(v, sees, half, acc); });
+                       [&](const char* v, bool sees) __attribute__((always_inline)) {
+#pragma unroll
+                         for (int i = 0; i < NE * 4; ++i) {
+                           const f32x4 z = special_values(v, out_col0(i >> 2, i & 3, half), sees);
+#pragma unroll
+                           for (int k = 0; k < 4; ++k) acc[i >> 2][(i & 3) * 4 + k] += z[k];
+                         }
+                       });
   }
   float l_tot = l_run + __shfl_xor(l_run, 32);
   int again = col;

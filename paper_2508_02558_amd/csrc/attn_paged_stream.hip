@@ -1,9 +1,11 @@
 // Attention over the paged cache, bf16, few query columns per KV head: single tokens and small trees.  Bound by memory: all a call does is read the keys
 // and values once.
 //
-// A workgroup takes 32 columns (paged_tile.h) and a share of their tiles.  Each wavefront streams tiles of its own straight into LDS, no barrier in
+// A workgroup takes 16 or 32 columns (paged_tile.h) and a share of their tiles.  Each wavefront streams tiles of its own straight into LDS, no barrier in
 // the loop: K of the next tile is requested as soon as this one's operands are in registers, V likewise, so that a wavefront has 8 to 16 KB under way at any time.
-// The pages of its next 64 tiles are looked up by one load, a tile per lane.  The wavefronts merge through LDS; splits of an item leave partials.
+// Where its next 64 tiles are is worked out at once, a tile per lane.  The wavefronts merge through LDS; splits of an item leave partials.
+#include <type_traits>
+
 #include "attn_paged_merge.h"
 #include "paged_tile_bf16.h"
 
@@ -13,27 +15,147 @@ namespace {
 
 constexpr int kStreamWaves = 8;   // most of a workgroup
 
+// 32 keys by C query columns on the matrix cores: K rows as the A operand of the logits, V columns through the transposing LDS read as that of the second
+// product, P^T as its B operand.  A tile of one tensor comes as HD / 16 fetches of 1 KB of consecutive LDS, each of whole rows in order; which 16-byte
+// piece of its row a lane brings is free: row r holds piece c of K in place c ^ k_turn(r), of V in place c ^ v_turn(r), which keeps the operand
+// reads off each other's banks.
 template <int HD>
-constexpr int stream_wave_lds() { return 2 * BfTile<HD>::kBytes + 256; }   // K, V and row statistics; the accumulators are parked where the tiles were
+struct Tile {
+  static constexpr int kRow = HD * 2, kBytes = kTileKeys * kRow;
+  static constexpr int kPieces = kRow / 16;             // of a row
+  static constexpr int kRowsPerFetch = kWave / kPieces, kFetches = kTileKeys / kRowsPerFetch;
+  static constexpr int NF = HD / 16;                    // K operands, V operands
+  typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+  static __device__ __forceinline__ i16x8 transposed(const uint8_t* lo, const uint8_t* hi) {
+    return __builtin_shufflevector(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)lo), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)hi), 0, 1, 2, 3, 4,
+                                   5, 6, 7);
+  }
+};
 
-template <int HD, int SEES>
-__global__ __launch_bounds__(kStreamWaves * kWave) __attribute__((amdgpu_waves_per_eu(2, 2)))
+template <int HD, int C>
+struct Math;
+
+// Fragments as in attn_tile_math.h: lane (col, half) holds keys 8 (i / 4) + 4 half + i % 4 of its column.
+template <int HD>
+struct Math<HD, 32> : Tile<HD> {
+  using T = Tile<HD>;
+  using Acc = f32x16;
+  static constexpr int NQ = HD / 16, NS = 16, NA = HD / 32, NB = 2, kSlots = NA * 4;
+  static __device__ __forceinline__ int k_turn(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
+  static __device__ __forceinline__ int v_turn(int r) { return HD == 128 ? (r & 3) << 2 : (r & 2) << 1; }
+  static __device__ __forceinline__ int key_base(int lane) { return 4 * (lane >> 5); }
+  static __device__ __forceinline__ int key(int i) { return 8 * (i >> 2) + (i & 3); }
+  static __device__ __forceinline__ int q_piece(int i, int lane) { return 2 * i + (lane >> 5); }
+  static __device__ __forceinline__ float over_row(float v, bool sum) {
+    const float o = __shfl_xor(v, 32);
+    return sum ? v + o : fmaxf(v, o);
+  }
+  static __device__ __forceinline__ void read_k(const uint8_t* tile, int lane, bf16x8 (&a)[T::NF]) {
+    const int half = lane >> 5, col = lane & 31;
+    const uint32_t at = (uint32_t)(col * T::kRow + ((half ^ k_turn(col)) << 4));
+#pragma unroll
+    for (int i = 0; i < T::NF; ++i) a[i] = *reinterpret_cast<const bf16x8*>(tile + (at ^ (uint32_t)(i * 32)));
+  }
+  static __device__ __forceinline__ void read_v(const uint8_t* tile, int lane, i16x8 (&f)[T::NF]) {
+    const int half = lane >> 5, grp = (lane >> 4) & 1, s16 = lane & 15, r = half * 4 + (s16 >> 2);
+    const uint32_t at = (uint32_t)(r * T::kRow + ((v_turn(r) << 4) ^ (grp * 32 + (s16 & 3) * 8)));
+#pragma unroll
+    for (int i = 0; i < T::NF; ++i) {
+      const uint8_t* from = tile + (at ^ (uint32_t)(i % NA * 64)) + i / NA * 16 * T::kRow;
+      f[i] = T::transposed(from, from + 8 * T::kRow);
+    }
+  }
+  static __device__ __forceinline__ void logits(const bf16x8 (&a)[T::NF], const bf16x8 (&q)[NQ], float (&s)[NS]) {
+    f32x16 c;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) c[i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], q[i], c, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = c[i];
+  }
+  static __device__ __forceinline__ void product(const i16x8 (&f)[T::NF], const bf16x8 (&pb)[NB], Acc (&acc)[NA]) {
+#pragma unroll
+    for (int i = 0; i < T::NF; ++i)
+      acc[i % NA] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[i]), pb[i / NA], acc[i % NA], 0, 0, 0);
+  }
+  // four results of consecutive channels, and the first of them
+  static __device__ __forceinline__ f32x4 slot(const Acc (&acc)[NA], int i) {
+    return {acc[i >> 2][(i & 3) * 4], acc[i >> 2][(i & 3) * 4 + 1], acc[i >> 2][(i & 3) * 4 + 2], acc[i >> 2][(i & 3) * 4 + 3]};
+  }
+  static __device__ __forceinline__ int channel(int i, int lane) { return out_col0(i >> 2, i & 3, lane >> 5); }
+};
+
+// 16 columns: half the work of a tile.  Row 4 q + r of half h of the logits is key 8 q + 4 h + r, so that lane (col, q) holds keys 8 q .. 8 q + 7 of its
+// column, as the second product takes them.
+template <int HD>
+struct Math<HD, 16> : Tile<HD> {
+  using T = Tile<HD>;
+  using Acc = f32x4;
+  static constexpr int NQ = HD / 32, NS = 8, NA = HD / 16, NB = 1, kSlots = NA;
+  static __device__ __forceinline__ int k_turn(int r) { return HD == 128 ? (r & 3) | (r >> 3) << 2 : ((r >> 1) & 1) | (r >> 3) << 1; }
+  static __device__ __forceinline__ int v_turn(int r) { return HD == 128 ? (r & 3) << 1 | (r & 8) : (r & 2) | (r & 8) >> 1; }
+  static __device__ __forceinline__ int key_base(int lane) { return 8 * (lane >> 4); }
+  static __device__ __forceinline__ int key(int i) { return i; }
+  static __device__ __forceinline__ int q_piece(int i, int lane) { return 4 * i + (lane >> 4); }
+  static __device__ __forceinline__ float over_row(float v, bool sum) {
+#pragma unroll
+    for (int o = 16; o < kWave; o <<= 1) {
+      const float x = __shfl_xor(v, o);
+      v = sum ? v + x : fmaxf(v, x);
+    }
+    return v;
+  }
+  static __device__ __forceinline__ void read_k(const uint8_t* tile, int lane, bf16x8 (&a)[T::NF]) {
+    const int q = lane >> 4, m = lane & 15, r = 8 * (m >> 2) + (m & 3);   // and r + 4, whose pieces turn alike
+    const uint32_t at = (uint32_t)(r * T::kRow + ((q ^ k_turn(r)) << 4));
+#pragma unroll
+    for (int i = 0; i < T::NF; ++i) a[i] = *reinterpret_cast<const bf16x8*>(tile + (at ^ (uint32_t)(i / 2 * 64)) + i % 2 * 4 * T::kRow);
+  }
+  static __device__ __forceinline__ void read_v(const uint8_t* tile, int lane, i16x8 (&f)[T::NF]) {
+    const int q = lane >> 4, s16 = lane & 15, r = 8 * q + (s16 >> 2);     // and r + 4
+    const uint32_t at = (uint32_t)(r * T::kRow + ((v_turn(r) << 4) ^ ((s16 & 3) * 8)));
+#pragma unroll
+    for (int i = 0; i < T::NF; ++i) {
+      const uint8_t* from = tile + (at ^ (uint32_t)(i * 32));
+      f[i] = T::transposed(from, from + 4 * T::kRow);
+    }
+  }
+  static __device__ __forceinline__ void logits(const bf16x8 (&a)[T::NF], const bf16x8 (&q)[NQ], float (&s)[NS]) {
+    f32x4 c[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int i = 0; i < T::NF; ++i) c[i % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], q[i / 2], c[i % 2], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) s[i] = c[i >> 2][i & 3];
+  }
+  static __device__ __forceinline__ void product(const i16x8 (&f)[T::NF], const bf16x8 (&pb)[NB], Acc (&acc)[NA]) {
+#pragma unroll
+    for (int i = 0; i < NA; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f[i]), pb[0], acc[i], 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 slot(const Acc (&acc)[NA], int i) { return acc[i]; }
+  static __device__ __forceinline__ int channel(int i, int lane) { return 16 * i + 4 * (lane >> 4); }
+};
+
+template <int HD, int C>
+constexpr int stream_wave_lds() { return 2 * Tile<HD>::kBytes + 2 * C * (int)sizeof(float); }   // K, V and row statistics; results are parked where the tiles were
+
+template <int HD, int C, int NW, int SEES>
+__global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void attn_paged_stream_kernel(const PagedAttnParams p) {
-  using T = BfTile<HD>;
-  constexpr int NE = T::NE, kSlots = NE * 4, kWaveLds = stream_wave_lds<HD>();
+  using T = Math<HD, C>;
+  constexpr int NS = T::NS, NA = T::NA, NF = T::NF, kSlots = T::kSlots, kRegs = sizeof(typename T::Acc) / 4, kWaveLds = stream_wave_lds<HD, C>();
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int nw = blockDim.x >> 6;
-  const int half = lane >> 5, col = lane & 31;
+  const int col = lane % C;
 
   PagedItem w;
   if (!find_item<SEES>(p, lane, w)) return;
   const int per_split = ceil_div(w.tiles, w.n_split);
   const int t_begin = min(w.tiles, w.split * per_split) + wave, t_end = min(w.tiles, (w.split + 1) * per_split);
-  const int n_mine = max(0, (t_end - t_begin + nw - 1) / nw);   // tiles t_begin, t_begin + nw, ...
+  const int n_mine = max(0, (t_end - t_begin + NW - 1) / NW);   // tiles t_begin, t_begin + NW, ...
 
-  const int column = w.blk * 32 + col, in = min(column, w.cols - 1);
+  const int column = w.blk * C + col, in = min(column, w.cols - 1);
   const int row = p.by_group.quotient(in), head = w.g * p.group + in - row * p.group;
   const RowSight sight = sight_of<SEES>(p, w, row);
 
@@ -41,7 +163,7 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   // tiles 64 i .. 64 i + 63 of this wavefront's, one per lane: where they are
   TilePlace places;
   auto look_up = [&](int j0) __attribute__((always_inline)) {
-    places = place_of<SEES>(p, w, item, tile_of<SEES>(p, w, min(t_begin + (j0 + lane) * nw, w.tiles - 1)));
+    places = place_of<SEES>(p, w, item, tile_of<SEES>(p, w, min(t_begin + (j0 + lane) * NW, w.tiles - 1)));
   };
 
   uint8_t* k_lds = smem + wave * kWaveLds;
@@ -74,15 +196,15 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
     }
   };
 
-  f32x16 acc[NE];
+  typename T::Acc acc[NA];
 #pragma unroll
-  for (int e = 0; e < NE; ++e)
+  for (int e = 0; e < NA; ++e)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[e][i] = 0.f;
+    for (int i = 0; i < kRegs; ++i) acc[e][i] = 0.f;
   float m_run = kNoMax, l_run = 0.f;
-  bf16x8 qf[T::NP], a[T::NP], pb[2];
-  i16x8 f[2 * NE];
-  f32x16 s;
+  bf16x8 qf[T::NQ], a[NF], pb[T::NB];
+  i16x8 f[NF];
+  float s[NS];
 
   // Requests in order: K(0), V(0), K(1), and then for each tile j K(j+2), V(j+1).  The waits count them.  Loads by the compiler in between (pages)
   // make a wait longer, never shorter.
@@ -98,12 +220,12 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   // logits of tile j, then the next K
   auto logits = [&](int j) __attribute__((always_inline)) {
     x = x_next;
-    T::read_k(k_lds, half, col, a);
+    T::read_k(k_lds, lane, a);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (j + 1 < n_mine) {
       if (((j + 1) & 63) == 0) look_up(j + 1);
       next = place_from(places, (j + 1) & 63);
-      x_next = tile_of<SEES>(p, w, t_begin + (j + 1) * nw);
+      x_next = tile_of<SEES>(p, w, t_begin + (j + 1) * NW);
       fetch(next, false, k_lds);
     }
     in_issue_order();
@@ -111,9 +233,35 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   };
   auto softmax = [&]() __attribute__((always_inline)) {
     full = x.full;
-    if (!full) mask_logits(s, seen_bits<SEES>(p, x, sight), half);
-    numerators<NE>(s, p.scale_log2, m_run, l_run, acc, pb);
+    if (!full) {
+      const uint32_t seen = seen_bits<SEES>(p, x, sight) >> T::key_base(lane);
+#pragma unroll
+      for (int i = 0; i < NS; ++i) s[i] = or_minus_infinity(s[i], bit_mask(seen, T::key(i)));
+    }
+    float m_loc = s[0];
+#pragma unroll
+    for (int i = 1; i < NS; ++i) m_loc = fmaxf(m_loc, s[i]);
+    m_loc *= p.scale_log2;
+    if (__ballot(m_loc > m_run + kRescaleSlack) != 0) {
+      const float m_new = fmaxf(m_run, T::over_row(m_loc, false));
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int e = 0; e < NA; ++e)
+#pragma unroll
+        for (int i = 0; i < kRegs; ++i) acc[e][i] *= alpha;
+    }
+    float l_loc = 0.f;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], p.scale_log2, -m_run));
+      l_loc += e;
+      pb[i >> 3][i & 7] = (__bf16)e;
+    }
+    l_run += l_loc;
   };
+
   if (n_mine > 0) {
     look_up(0);
     x_next = tile_of<SEES>(p, w, t_begin);
@@ -124,7 +272,7 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
     in_issue_order();
     const u32x4* q = reinterpret_cast<const u32x4*>((const char*)p.q + 2 * (w.b * p.q_sb + head * p.q_sh + row * p.q_sr));
 #pragma unroll
-    for (int i = 0; i < T::NP; ++i) qf[i] = __builtin_bit_cast(bf16x8, q[i * 2 + half]);
+    for (int i = 0; i < T::NQ; ++i) qf[i] = __builtin_bit_cast(bf16x8, q[T::q_piece(i, lane)]);
     // logits of tile j, second product of tile j - 1, softmax of tile j
 #pragma clang loop unroll(disable)
     for (int j = 0; j <= n_mine; ++j) {
@@ -140,7 +288,7 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
         if (j < n_mine) fetch(of_v, true, v_lds);
         in_issue_order();
         if (!full) specials |= take_specials(f);
-        T::pv(f, pb, acc);
+        T::product(f, pb, acc);
         __builtin_amdgcn_sched_barrier(0);
       }
       if (j < n_mine) softmax();
@@ -148,73 +296,95 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   }
 
   if (specials)
-    add_specials<SEES>(p, w, sight, 2, 0, n_mine, [&](int j) { return t_begin + j * nw; },
-                       [&](const char* v, bool sees) __attribute__((always_inline)) { add_special_row<NE>(v, sees, half, acc); });
-  const float l_tot = l_run + __shfl_xor(l_run, 32);
-  // Merge: every wavefront parks its accumulators (slot i of a lane in place i ^ its turn) and its columns' statistics; they then share out the slots.
-  auto turn = [](int l) { return HD == 128 ? l & 15 : (l >> 1) & 7; };
+    add_specials<SEES>(p, w, sight, 2, 0, n_mine, [&](int j) { return t_begin + j * NW; }, [&](const char* v, bool sees) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kSlots; ++i) {
+        const f32x4 z = special_values(v, T::channel(i, lane), sees);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[C == 32 ? i >> 2 : i][C == 32 ? (i & 3) * 4 + k : k] += z[k];
+      }
+    });
+  const float l_tot = T::over_row(l_run, true);
+  // Merge: every wavefront parks its results (slot i of a lane in place i ^ its turn) and its columns' statistics; they then share out the slots, with
+  // everything that a slot needs requested at once.
+  auto parked = [&](int k, int i) __attribute__((always_inline)) {
+    return reinterpret_cast<f32x4*>(smem + k * kWaveLds + lane * kSlots * 16 + ((i ^ (kSlots == 16 ? lane & 15 : kSlots == 8 ? (lane >> 1) & 7 : (lane >> 2) & 3)) << 4));
+  };
   auto stat_of = [&](int k) __attribute__((always_inline)) { return reinterpret_cast<float*>(smem + k * kWaveLds + 2 * T::kBytes); };
 #pragma unroll
-  for (int e = 0; e < NE; ++e)
-#pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4) {
-      const f32x4 v = {acc[e][i4 * 4], acc[e][i4 * 4 + 1], acc[e][i4 * 4 + 2], acc[e][i4 * 4 + 3]};
-      *reinterpret_cast<f32x4*>(k_lds + lane * kSlots * 16 + (((e * 4 + i4) ^ turn(lane)) << 4)) = v;
-    }
-  if (lane < 32) { stat_of(wave)[lane] = m_run; stat_of(wave)[32 + lane] = l_tot; }
+  for (int i = 0; i < kSlots; ++i) *parked(wave, i) = T::slot(acc, i);
+  if (lane < C) { stat_of(wave)[lane] = m_run; stat_of(wave)[C + lane] = l_tot; }
   __syncthreads();
-  float f_w[kStreamWaves], m_tot = kNoMax, l_all = 0.f;
+  constexpr int kMine = kSlots / NW > 0 ? kSlots / NW : 1;
+  if (kSlots < NW && wave >= kSlots) return;
+  float f_w[NW], l_w[NW], m_tot = kNoMax, l_all = 0.f;
+  f32x4 part[kMine][NW];
 #pragma unroll
-  for (int k = 0; k < kStreamWaves; ++k) {
-    f_w[k] = k < nw ? stat_of(k)[col] : kNoMax;
-    m_tot = fmaxf(m_tot, f_w[k]);
+  for (int k = 0; k < NW; ++k) {
+    f_w[k] = stat_of(k)[col];
+    l_w[k] = stat_of(k)[C + col];
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) part[j][k] = *parked(k, wave + j * NW);
   }
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int k = 0; k < kStreamWaves; ++k)
-    if (k < nw) {
-      f_w[k] = __builtin_amdgcn_exp2f(f_w[k] - m_tot);   // a wavefront that saw no tile parked (kNoMax, 0, 0)
-      l_all += f_w[k] * stat_of(k)[32 + col];
-    }
+  for (int k = 0; k < NW; ++k) m_tot = fmaxf(m_tot, f_w[k]);
+#pragma unroll
+  for (int k = 0; k < NW; ++k) {
+    f_w[k] = __builtin_amdgcn_exp2f(f_w[k] - m_tot);   // a wavefront that saw no tile parked (kNoMax, 0, 0)
+    l_all += f_w[k] * l_w[k];
+  }
   const float inv = 1.f / l_all;
-  if (column < w.cols) {
-    for (int i = wave; i < kSlots; i += nw) {
-      f32x4 o4 = {0.f, 0.f, 0.f, 0.f};
+  if (column >= w.cols) return;
 #pragma unroll
-      for (int k = 0; k < kStreamWaves; ++k)
-        if (k < nw) o4 += *reinterpret_cast<const f32x4*>(smem + k * kWaveLds + lane * kSlots * 16 + ((i ^ turn(lane)) << 4)) * f_w[k];
-      const int d0 = out_col0(i >> 2, i & 3, half);
-      if (w.n_split > 1) {
-        *reinterpret_cast<f32x4*>(p.part_o + ((int64_t)w.slot * 32 + col) * HD + d0) = o4;
-      } else {
-        bf16x4 ob;
+  for (int j = 0; j < kMine; ++j) {
+    f32x4 o4 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int r = 0; r < 4; ++r) ob[r] = (__bf16)(sight.none ? 0.f : o4[r] * inv);
-        *reinterpret_cast<bf16x4*>((__bf16*)p.out + w.b * p.o_sb + head * p.o_sh + row * p.o_sr + d0) = ob;
-      }
+    for (int k = 0; k < NW; ++k) o4 += part[j][k] * f_w[k];
+    const int d0 = T::channel(wave + j * NW, lane);
+    if (w.n_split > 1) {
+      *reinterpret_cast<f32x4*>(p.part_o + ((int64_t)w.slot * C + col) * HD + d0) = o4;
+    } else {
+      bf16x4 ob;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) ob[r] = (__bf16)(sight.none ? 0.f : o4[r] * inv);
+      *reinterpret_cast<bf16x4*>((__bf16*)p.out + w.b * p.o_sb + head * p.o_sh + row * p.o_sr + d0) = ob;
     }
-    if (w.n_split > 1 && wave == 0 && lane < 32) {
-      p.part_ml[(int64_t)w.slot * 64 + lane] = sight.none ? -INFINITY : m_tot;
-      p.part_ml[(int64_t)w.slot * 64 + 32 + lane] = l_all;
-    }
+  }
+  if (w.n_split > 1 && wave == 0 && lane < C) {
+    p.part_ml[(int64_t)w.slot * 2 * C + lane] = sight.none ? -INFINITY : m_tot;
+    p.part_ml[(int64_t)w.slot * 2 * C + C + lane] = l_all;
   }
 }
 
-template <int HD, int SEES>
+template <int HD, int C, int NW, int SEES>
 hipError_t launch_sees(const PagedAttnParams& p, const PagedPlan& pl, hipStream_t s) {
   static LdsOptIn lds;
-  const auto kernel = attn_paged_stream_kernel<HD, SEES>;
-  hipError_t e = lds.ensure(reinterpret_cast<const void*>(kernel), kStreamWaves * stream_wave_lds<HD>());
+  const auto kernel = attn_paged_stream_kernel<HD, C, NW, SEES>;
+  constexpr int kLds = NW * stream_wave_lds<HD, C>();
+  hipError_t e = lds.ensure(reinterpret_cast<const void*>(kernel), kLds);
   if (e != hipSuccess) return e;
-  if (pl.waves < 1 || pl.waves > kStreamWaves || p.block_cols != 32) return hipErrorInvalidValue;
-  e = launch(kernel, dim3((unsigned)p.workgroups), dim3(pl.waves * kWave), pl.waves * stream_wave_lds<HD>(), s, p);
+  e = launch(kernel, dim3((unsigned)p.workgroups), dim3(NW * kWave), kLds, s, p);
   return e != hipSuccess || !pl.splits ? e : launch_paged_merge<__bf16, HD>(p, s);
+}
+
+template <int HD, int C>
+hipError_t launch_cols(const PagedAttnParams& p, const PagedPlan& pl, int sees, hipStream_t s) {
+  if (pl.waves == 8) return sees == kSeeTree ? launch_sees<HD, C, 8, kSeeTree>(p, pl, s) : launch_sees<HD, C, 8, kSeeWindow>(p, pl, s);
+  if (pl.waves != 4) return hipErrorInvalidValue;
+  return sees == kSeeTree ? launch_sees<HD, C, 4, kSeeTree>(p, pl, s) : launch_sees<HD, C, 4, kSeeWindow>(p, pl, s);
+}
+
+template <int HD>
+hipError_t launch_dim(const PagedAttnParams& p, const PagedPlan& pl, int sees, hipStream_t s) {
+  return p.block_cols == 16 ? launch_cols<HD, 16>(p, pl, sees, s) : launch_cols<HD, 32>(p, pl, sees, s);
 }
 
 }  // namespace
 
 hipError_t launch_attn_paged_stream(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s) {
-  if (d == 128) return sees == kSeeTree ? launch_sees<128, kSeeTree>(p, pl, s) : launch_sees<128, kSeeWindow>(p, pl, s);
-  return sees == kSeeTree ? launch_sees<64, kSeeTree>(p, pl, s) : launch_sees<64, kSeeWindow>(p, pl, s);
+  if (p.block_cols != 16 && p.block_cols != 32) return hipErrorInvalidValue;
+  return d == 128 ? launch_dim<128>(p, pl, sees, s) : launch_dim<64>(p, pl, sees, s);
 }
 
 }  // namespace sdllm

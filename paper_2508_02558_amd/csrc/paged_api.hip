@@ -53,7 +53,7 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   const int64_t cols = (int64_t)s.rows * (s.n_q_heads / s.n_kv_heads);
   pl = PagedPlan{};
   pl.kernel = s.dtype == SDLLM_F32 ? kPagedF32 : cols <= 32 ? kPagedStream : kPagedShared;
-  pl.block_cols = pl.kernel == kPagedF32 ? kGeneralRowsF32 : pl.kernel == kPagedStream ? 32 : cols <= 128 ? 128 : 256;
+  pl.block_cols = pl.kernel == kPagedF32 ? kGeneralRowsF32 : pl.kernel == kPagedStream ? (cols <= 16 ? 16 : 32) : cols <= 128 ? 128 : 256;
   // columns, blocks and threads of a launch (the merge's too) are counted in 32 bits
   if (cols > INT32_MAX - 256) return SDLLM_ERR_UNSUPPORTED;
   pl.max_blocks = (int)((cols + pl.block_cols - 1) / pl.block_cols);

@@ -1,60 +1,10 @@
-// bf16 tiles of the paged cache in LDS, and what the matrix cores take of them: 32 keys by 32 query columns, fragments as in attn_tile_math.h (K rows as
-// the A operand of the logits, V columns through the transposing LDS read, P^T as the B operand), for head_dim 64 and 128.
-//
-// A tile of one tensor comes as HD / 16 fetches of 1 KB of consecutive LDS, each of whole rows in order; which 16-byte piece of its row a lane brings is free, so
-// the pieces of a row are permuted to keep the operand reads off each other's banks.
+// What the bf16 kernels of the paged cache's attention share: masks, the softmax reference, values that are no numbers, and where a tile's rows are.
 #pragma once
 
 #include "attn_tile_math.h"
 #include "paged_tile.h"
 
 namespace sdllm {
-
-template <int HD>
-struct BfTile {
-  static constexpr int kRow = HD * 2, kBytes = kTileKeys * kRow;
-  static constexpr int kPieces = kRow / 16;             // of a row
-  static constexpr int kRowsPerFetch = kWave / kPieces;
-  static constexpr int kFetches = kTileKeys / kRowsPerFetch;
-  static constexpr int NP = HD / 16;                    // operands of the logits
-  static constexpr int NE = HD / 32;                    // accumulators
-  // row r holds piece c of K in place c ^ k_turn(r), of V in place c ^ v_turn(r)
-  static __device__ __forceinline__ int k_turn(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
-  static __device__ __forceinline__ int v_turn(int r) { return HD == 128 ? (r & 3) << 2 : (r & 2) << 1; }
-
-  static __device__ __forceinline__ void read_k(const uint8_t* tile, int half, int col, bf16x8 (&a)[NP]) {
-    const uint32_t at = (uint32_t)(col * kRow + ((half ^ k_turn(col)) << 4));
-#pragma unroll
-    for (int i = 0; i < NP; ++i) a[i] = *reinterpret_cast<const bf16x8*>(tile + (at ^ (uint32_t)(i * 32)));
-  }
-  static __device__ __forceinline__ void read_v(const uint8_t* tile, int lane, i16x8 (&f)[2 * NE]) {
-    typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-    const int half = lane >> 5, grp = (lane >> 4) & 1, s16 = lane & 15, r = half * 4 + (s16 >> 2);
-    const uint32_t at = (uint32_t)(r * kRow + ((v_turn(r) << 4) ^ (grp * 32 + (s16 & 3) * 8)));
-#pragma unroll
-    for (int st = 0; st < 2; ++st)
-#pragma unroll
-      for (int e = 0; e < NE; ++e) {
-        const uint8_t* from = tile + (at ^ (uint32_t)(e * 64)) + st * 16 * kRow;
-        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)from);
-        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(from + 8 * kRow));
-        f[st * NE + e] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-  }
-  static __device__ __forceinline__ void logits(const bf16x8 (&a)[NP], const bf16x8 (&qf)[NP], f32x16& s) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], qf[i], s, 0, 0, 0);
-  }
-  static __device__ __forceinline__ void pv(const i16x8 (&f)[2 * NE], const bf16x8 (&pb)[2], f32x16 (&acc)[NE]) {
-#pragma unroll
-    for (int st = 0; st < 2; ++st)
-#pragma unroll
-      for (int e = 0; e < NE; ++e)
-        acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[st * NE + e]), pb[st], acc[e], 0, 0, 0);
-  }
-};
 
 // Logits of keys that a row does not see become -inf; `seen` is the row's bits of the tile (seen_bits).
 __device__ __forceinline__ void mask_logits(f32x16& s, uint32_t seen, int half) {
@@ -63,9 +13,8 @@ __device__ __forceinline__ void mask_logits(f32x16& s, uint32_t seen, int half) 
   for (int i = 0; i < 16; ++i) s[i] = or_minus_infinity(s[i], bit_mask(seen, 8 * (i >> 2) + (i & 3)));
 }
 
-// Softmax numerators of a tile's raw logits as the B operands of the second product, against a reference that moves when a maximum exceeds it by
-// more than kRescaleSlack (attn_tile_math.h).  Rounded to bf16, the type of what they multiply: half a step, 2^-8, of each numerator,
-// as much as the rounding of the result.
+// The softmax reference of a row moves when a maximum exceeds it by more than kRescaleSlack (attn_tile_math.h).  Numerators against it are rounded to bf16, the
+// type of what they multiply: half a step, 2^-8, of each, as much as the rounding of the result.
 template <int NE>
 __device__ __forceinline__ void move_reference_to(float m_loc, float& m_ref, float& l_run, f32x16 (&acc)[NE]) {
   if (__ballot(m_loc > m_ref + kRescaleSlack) != 0) {
@@ -78,22 +27,6 @@ __device__ __forceinline__ void move_reference_to(float m_loc, float& m_ref, flo
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[e][i] *= alpha;
   }
-}
-
-template <int NE>
-__device__ __forceinline__ void numerators(const f32x16& s, float scale_log2, float& m_ref, float& l_run, f32x16 (&acc)[NE], bf16x8 (&pb)[2]) {
-  float m_loc = s[0];
-#pragma unroll
-  for (int i = 1; i < 16; ++i) m_loc = fmaxf(m_loc, s[i]);
-  move_reference_to<NE>(m_loc * scale_log2, m_ref, l_run, acc);
-  float l_loc = 0.f;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale_log2, -m_ref));
-    l_loc += x;
-    pb[i >> 3][i & 7] = (__bf16)x;
-  }
-  l_run += l_loc;
 }
 
 // Takes values that are no numbers out of a masked tile's operands (paged_tile.h), two values a word; true for all lanes if there are any.
@@ -119,17 +52,13 @@ __device__ __forceinline__ bool take_specials(i16x8 (&f)[N]) {
   return true;
 }
 
-// add_specials' share of one row of V
-template <int NE>
-__device__ __forceinline__ void add_special_row(const char* v, bool sees, int half, f32x16 (&acc)[NE]) {
+// add_specials' share of four channels of a row of V
+__device__ __forceinline__ f32x4 special_values(const char* v, int channel, bool sees) {
+  const bf16x4 u = *reinterpret_cast<const bf16x4*>(v + 2 * channel);
+  f32x4 z;
 #pragma unroll
-  for (int e = 0; e < NE; ++e)
-#pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4) {
-      const bf16x4 u = *reinterpret_cast<const bf16x4*>(v + 2 * out_col0(e, i4, half));
-#pragma unroll
-      for (int k = 0; k < 4; ++k) acc[e][i4 * 4 + k] += sees && !(fabsf((float)u[k]) < INFINITY) ? (float)u[k] : 0.f;
-    }
+  for (int k = 0; k < 4; ++k) z[k] = sees && !(fabsf((float)u[k]) < INFINITY) ? (float)u[k] : 0.f;
+  return z;
 }
 
 // Where the rows of an item are (bf16), in bytes: its pages' and its own (kSeeTree) rows of the KV head
