@@ -10,7 +10,7 @@
 #include <type_traits>
 
 #include "attn_paged_merge.h"
-#include "paged_tile_bf16.h"
+#include "paged_place.h"
 
 namespace sdllm {
 
@@ -120,7 +120,7 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
       for (int i = 0; i < NP; ++i) qf[i] = __builtin_bit_cast(bf16x8, q[i * 2 + half]);
     }
     // Tiles 64 i .. 64 i + 63 of the share, one per lane: where they are, and which of them and of the 64 before every row of this wave sees whole
-    const ItemBase item = item_base<SEES>(p, w);
+    const ItemBase item = item_base<2, SEES>(p, w);
     TilePlace places;
     uint64_t whole_now = 0, whole_before = 0;
     int at_hand = 0;
@@ -332,7 +332,7 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
                        [&](const char* v, bool sees) __attribute__((always_inline)) {
 #pragma unroll
                          for (int i = 0; i < NE * 4; ++i) {
-                           const f32x4 z = special_values(v, out_col0(i >> 2, i & 3, half), sees);
+                           const f32x4 z = special_values<__bf16>(v, out_col0(i >> 2, i & 3, half), sees);
 #pragma unroll
                            for (int k = 0; k < 4; ++k) acc[i >> 2][(i & 3) * 4 + k] += z[k];
                          }

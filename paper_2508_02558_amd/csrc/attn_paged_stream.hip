@@ -1,5 +1,5 @@
-// Attention over the paged cache, bf16, few query columns per KV head: single tokens and small trees.  Bound by memory: all a call does is read the keys
-// and values once.
+// Attention over the paged cache, for few query columns per KV head, single tokens and small trees, and for fp32 tensors.  Bound by memory with bf16
+// tensors: all a call does is read the keys and values once.  With fp32 tensors, exact products and sums, by the matrix cores, which take sixteen times as long.
 //
 // A workgroup takes 16 or 32 columns (paged_tile.h) and a share of their tiles.  Each wavefront streams tiles of its own straight into LDS, no barrier in
 // the loop: K of the next tile is requested as soon as this one's operands are in registers, V likewise, so that a wavefront has 8 to 16 KB under way at any time.
@@ -7,40 +7,42 @@
 #include <type_traits>
 
 #include "attn_paged_merge.h"
-#include "paged_tile_bf16.h"
+#include "paged_place.h"
 
 namespace sdllm {
 
 namespace {
 
-constexpr int kStreamWaves = 8;   // most of a workgroup
-
-// 32 keys by C query columns on the matrix cores: K rows as the A operand of the logits, V columns through the transposing LDS read as that of the second
-// product, P^T as its B operand.  A tile of one tensor comes as HD / 16 fetches of 1 KB of consecutive LDS, each of whole rows in order; which 16-byte
+// 32 keys by C query columns of tensors of type E on the matrix cores: K rows as the A operand of the logits, V columns through the transposing LDS read as that of the second
+// product, P^T as its B operand.  A tile of one tensor comes as fetches of 1 KB of consecutive LDS, each of whole rows in order; which 16-byte
 // piece of its row a lane brings is free: row r holds piece c of K in place c ^ k_turn(r), of V in place c ^ v_turn(r), which keeps the operand
 // reads off each other's banks.
-template <int HD>
+template <typename E, int HD>
 struct Tile {
-  static constexpr int kRow = HD * 2, kBytes = kTileKeys * kRow;
+  static constexpr int kRow = HD * (int)sizeof(E), kBytes = kTileKeys * kRow;
   static constexpr int kPieces = kRow / 16;             // of a row
   static constexpr int kRowsPerFetch = kWave / kPieces, kFetches = kTileKeys / kRowsPerFetch;
-  static constexpr int NF = HD / 16;                    // K operands, V operands
-  typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-  static __device__ __forceinline__ i16x8 transposed(const uint8_t* lo, const uint8_t* hi) {
-    return __builtin_shufflevector(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)lo), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)hi), 0, 1, 2, 3, 4,
-                                   5, 6, 7);
-  }
 };
 
-template <int HD, int C>
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+__device__ __forceinline__ i16x8 transposed(const uint8_t* lo, const uint8_t* hi) {
+  return __builtin_shufflevector(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)lo), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)hi), 0, 1, 2, 3, 4, 5,
+                                 6, 7);
+}
+
+template <typename E, int HD, int C>
 struct Math;
 
 // Fragments as in attn_tile_math.h: lane (col, half) holds keys 8 (i / 4) + 4 half + i % 4 of its column.
 template <int HD>
-struct Math<HD, 32> : Tile<HD> {
-  using T = Tile<HD>;
+struct Math<__bf16, HD, 32> : Tile<__bf16, HD> {
+  using T = Tile<__bf16, HD>;
+  using Q = bf16x8;
+  using K = bf16x8;
+  using V = i16x8;
+  using P = bf16x8;
   using Acc = f32x16;
-  static constexpr int NQ = HD / 16, NS = 16, NA = HD / 32, NB = 2, kSlots = NA * 4;
+  static constexpr int NQ = HD / 16, NK = HD / 16, NV = HD / 16, NS = 16, NA = HD / 32, NB = 2, kSlots = NA * 4;
   static __device__ __forceinline__ int k_turn(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
   static __device__ __forceinline__ int v_turn(int r) { return HD == 128 ? (r & 3) << 2 : (r & 2) << 1; }
   static __device__ __forceinline__ int key_base(int lane) { return 4 * (lane >> 5); }
@@ -50,22 +52,22 @@ struct Math<HD, 32> : Tile<HD> {
     const float o = __shfl_xor(v, 32);
     return sum ? v + o : fmaxf(v, o);
   }
-  static __device__ __forceinline__ void read_k(const uint8_t* tile, int lane, bf16x8 (&a)[T::NF]) {
+  static __device__ __forceinline__ void read_k(const uint8_t* tile, int lane, bf16x8 (&a)[NK]) {
     const int half = lane >> 5, col = lane & 31;
     const uint32_t at = (uint32_t)(col * T::kRow + ((half ^ k_turn(col)) << 4));
 #pragma unroll
-    for (int i = 0; i < T::NF; ++i) a[i] = *reinterpret_cast<const bf16x8*>(tile + (at ^ (uint32_t)(i * 32)));
+    for (int i = 0; i < NK; ++i) a[i] = *reinterpret_cast<const bf16x8*>(tile + (at ^ (uint32_t)(i * 32)));
   }
-  static __device__ __forceinline__ void read_v(const uint8_t* tile, int lane, i16x8 (&f)[T::NF]) {
+  static __device__ __forceinline__ void read_v(const uint8_t* tile, int lane, i16x8 (&f)[NV]) {
     const int half = lane >> 5, grp = (lane >> 4) & 1, s16 = lane & 15, r = half * 4 + (s16 >> 2);
     const uint32_t at = (uint32_t)(r * T::kRow + ((v_turn(r) << 4) ^ (grp * 32 + (s16 & 3) * 8)));
 #pragma unroll
-    for (int i = 0; i < T::NF; ++i) {
+    for (int i = 0; i < NV; ++i) {
       const uint8_t* from = tile + (at ^ (uint32_t)(i % NA * 64)) + i / NA * 16 * T::kRow;
-      f[i] = T::transposed(from, from + 8 * T::kRow);
+      f[i] = transposed(from, from + 8 * T::kRow);
     }
   }
-  static __device__ __forceinline__ void logits(const bf16x8 (&a)[T::NF], const bf16x8 (&q)[NQ], float (&s)[NS]) {
+  static __device__ __forceinline__ void logits(const bf16x8 (&a)[NK], const bf16x8 (&q)[NQ], float (&s)[NS]) {
     f32x16 c;
 #pragma unroll
     for (int i = 0; i < 16; ++i) c[i] = 0.f;
@@ -74,14 +76,18 @@ struct Math<HD, 32> : Tile<HD> {
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = c[i];
   }
-  static __device__ __forceinline__ void product(const i16x8 (&f)[T::NF], const bf16x8 (&pb)[NB], Acc (&acc)[NA]) {
+  static __device__ __forceinline__ void product(const i16x8 (&f)[NV], const bf16x8 (&pb)[NB], Acc (&acc)[NA]) {
 #pragma unroll
-    for (int i = 0; i < T::NF; ++i)
+    for (int i = 0; i < NV; ++i)
       acc[i % NA] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[i]), pb[i / NA], acc[i % NA], 0, 0, 0);
   }
-  // four results of consecutive channels, and the first of them
+  // slot i: four results of consecutive channels, the first of them channel()
   static __device__ __forceinline__ f32x4 slot(const Acc (&acc)[NA], int i) {
     return {acc[i >> 2][(i & 3) * 4], acc[i >> 2][(i & 3) * 4 + 1], acc[i >> 2][(i & 3) * 4 + 2], acc[i >> 2][(i & 3) * 4 + 3]};
+  }
+  static __device__ __forceinline__ void add(Acc (&acc)[NA], int i, const f32x4& z) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[i >> 2][(i & 3) * 4 + k] += z[k];
   }
   static __device__ __forceinline__ int channel(int i, int lane) { return out_col0(i >> 2, i & 3, lane >> 5); }
 };
@@ -89,10 +95,14 @@ struct Math<HD, 32> : Tile<HD> {
 // 16 columns: half the work of a tile.  Row 4 q + r of half h of the logits is key 8 q + 4 h + r, so that lane (col, q) holds keys 8 q .. 8 q + 7 of its
 // column, as the second product takes them.
 template <int HD>
-struct Math<HD, 16> : Tile<HD> {
-  using T = Tile<HD>;
+struct Math<__bf16, HD, 16> : Tile<__bf16, HD> {
+  using T = Tile<__bf16, HD>;
+  using Q = bf16x8;
+  using K = bf16x8;
+  using V = i16x8;
+  using P = bf16x8;
   using Acc = f32x4;
-  static constexpr int NQ = HD / 32, NS = 8, NA = HD / 16, NB = 1, kSlots = NA;
+  static constexpr int NQ = HD / 32, NK = HD / 16, NV = HD / 16, NS = 8, NA = HD / 16, NB = 1, kSlots = NA;
   static __device__ __forceinline__ int k_turn(int r) { return HD == 128 ? (r & 3) | (r >> 3) << 2 : ((r >> 1) & 1) | (r >> 3) << 1; }
   static __device__ __forceinline__ int v_turn(int r) { return HD == 128 ? (r & 3) << 1 | (r & 8) : (r & 2) | (r & 8) >> 1; }
   static __device__ __forceinline__ int key_base(int lane) { return 8 * (lane >> 4); }
@@ -106,44 +116,101 @@ struct Math<HD, 16> : Tile<HD> {
     }
     return v;
   }
-  static __device__ __forceinline__ void read_k(const uint8_t* tile, int lane, bf16x8 (&a)[T::NF]) {
+  static __device__ __forceinline__ void read_k(const uint8_t* tile, int lane, bf16x8 (&a)[NK]) {
     const int q = lane >> 4, m = lane & 15, r = 8 * (m >> 2) + (m & 3);   // and r + 4, whose pieces turn alike
     const uint32_t at = (uint32_t)(r * T::kRow + ((q ^ k_turn(r)) << 4));
 #pragma unroll
-    for (int i = 0; i < T::NF; ++i) a[i] = *reinterpret_cast<const bf16x8*>(tile + (at ^ (uint32_t)(i / 2 * 64)) + i % 2 * 4 * T::kRow);
+    for (int i = 0; i < NK; ++i) a[i] = *reinterpret_cast<const bf16x8*>(tile + (at ^ (uint32_t)(i / 2 * 64)) + i % 2 * 4 * T::kRow);
   }
-  static __device__ __forceinline__ void read_v(const uint8_t* tile, int lane, i16x8 (&f)[T::NF]) {
+  static __device__ __forceinline__ void read_v(const uint8_t* tile, int lane, i16x8 (&f)[NV]) {
     const int q = lane >> 4, s16 = lane & 15, r = 8 * q + (s16 >> 2);     // and r + 4
     const uint32_t at = (uint32_t)(r * T::kRow + ((v_turn(r) << 4) ^ ((s16 & 3) * 8)));
 #pragma unroll
-    for (int i = 0; i < T::NF; ++i) {
+    for (int i = 0; i < NV; ++i) {
       const uint8_t* from = tile + (at ^ (uint32_t)(i * 32));
-      f[i] = T::transposed(from, from + 4 * T::kRow);
+      f[i] = transposed(from, from + 4 * T::kRow);
     }
   }
-  static __device__ __forceinline__ void logits(const bf16x8 (&a)[T::NF], const bf16x8 (&q)[NQ], float (&s)[NS]) {
+  static __device__ __forceinline__ void logits(const bf16x8 (&a)[NK], const bf16x8 (&q)[NQ], float (&s)[NS]) {
     f32x4 c[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int i = 0; i < T::NF; ++i) c[i % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], q[i / 2], c[i % 2], 0, 0, 0);
+    for (int i = 0; i < NK; ++i) c[i % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], q[i / 2], c[i % 2], 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < NS; ++i) s[i] = c[i >> 2][i & 3];
   }
-  static __device__ __forceinline__ void product(const i16x8 (&f)[T::NF], const bf16x8 (&pb)[NB], Acc (&acc)[NA]) {
+  static __device__ __forceinline__ void product(const i16x8 (&f)[NV], const bf16x8 (&pb)[NB], Acc (&acc)[NA]) {
 #pragma unroll
     for (int i = 0; i < NA; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f[i]), pb[0], acc[i], 0, 0, 0);
   }
   static __device__ __forceinline__ f32x4 slot(const Acc (&acc)[NA], int i) { return acc[i]; }
+  static __device__ __forceinline__ void add(Acc (&acc)[NA], int i, const f32x4& z) { acc[i] += z; }
   static __device__ __forceinline__ int channel(int i, int lane) { return 16 * i + 4 * (lane >> 4); }
 };
 
-template <int HD, int C>
-constexpr int stream_wave_lds() { return 2 * Tile<HD>::kBytes + 2 * C * (int)sizeof(float); }   // K, V and row statistics; results are parked where the tiles were
+// fp32: lane (col, part) holds keys 16 (i / 4) + 4 part + i % 4 of its column.  The order in which channels are contracted is free: a 16-byte piece of a row is
+// four operands, of the logits four channels of a key, of the second product four columns of V, so that results are columns 64 c + 4 m + e for row m of product 4 c + e.
+template <int HD>
+struct Math<float, HD, 16> : Tile<float, HD> {
+  using T = Tile<float, HD>;
+  using Q = f32x4;
+  using K = f32x4;
+  using V = f32x4;
+  using P = f32x4;
+  using Acc = f32x4;
+  static constexpr int NQ = HD / 16, NK = HD / 8, NV = HD / 8, NS = 8, NA = HD / 16, NB = 2, kSlots = NA;
+  static __device__ __forceinline__ int k_turn(int r) { return r & 15; }
+  static __device__ __forceinline__ int v_turn(int) { return 0; }
+  static __device__ __forceinline__ int key_base(int lane) { return 4 * (lane >> 4); }
+  static __device__ __forceinline__ int key(int i) { return 16 * (i >> 2) + (i & 3); }
+  static __device__ __forceinline__ int q_piece(int i, int lane) { return 4 * i + (lane >> 4); }
+  static __device__ __forceinline__ float over_row(float v, bool sum) { return Math<__bf16, HD, 16>::over_row(v, sum); }
+  static __device__ __forceinline__ void read_k(const uint8_t* tile, int lane, f32x4 (&a)[NK]) {
+    const int part = lane >> 4, col = lane & 15;
+    const uint32_t at = (uint32_t)(col * T::kRow + ((part ^ k_turn(col)) << 4));
+#pragma unroll
+    for (int i = 0; i < NK; ++i) a[i] = *reinterpret_cast<const f32x4*>(tile + (at ^ (uint32_t)(i / 2 * 64)) + i % 2 * 16 * T::kRow);   // keys col and 16 + col
+  }
+  static __device__ __forceinline__ void read_v(const uint8_t* tile, int lane, f32x4 (&f)[NV]) {
+    const uint8_t* from = tile + 4 * (lane >> 4) * T::kRow + (lane & 15) * 16;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) f[i] = *reinterpret_cast<const f32x4*>(from + key(i & 7) * T::kRow + (i >> 3) * 256);
+  }
+  static __device__ __forceinline__ void logits(const f32x4 (&a)[NK], const f32x4 (&q)[NQ], float (&s)[NS]) {
+    f32x4 c[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int t = 0; t < NQ; ++t)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) c[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[2 * t + h][k], q[t][k], c[h], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) s[i] = c[i >> 2][i & 3];
+  }
+  static __device__ __forceinline__ void product(const f32x4 (&f)[NV], const f32x4 (&pb)[NB], Acc (&acc)[NA]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < NA; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[(e >> 2) * 8 + i][e & 3], pb[i >> 2][i & 3], acc[e], 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 slot(const Acc (&acc)[NA], int i) {
+    const int e = i & ~3, r = i & 3;
+    return {acc[e][r], acc[e + 1][r], acc[e + 2][r], acc[e + 3][r]};
+  }
+  static __device__ __forceinline__ void add(Acc (&acc)[NA], int i, const f32x4& z) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[(i & ~3) + k][i & 3] += z[k];
+  }
+  static __device__ __forceinline__ int channel(int i, int lane) { return 64 * (i >> 2) + 16 * (lane >> 4) + 4 * (i & 3); }
+};
 
-template <int HD, int C, int NW, int SEES>
+template <typename E, int HD, int C>
+constexpr int stream_wave_lds() { return 2 * Tile<E, HD>::kBytes + 2 * C * (int)sizeof(float); }   // K, V and row statistics; results are parked where the tiles were
+
+template <typename E, int HD, int C, int NW, int SEES>
 __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void attn_paged_stream_kernel(const PagedAttnParams p) {
-  using T = Math<HD, C>;
-  constexpr int NS = T::NS, NA = T::NA, NF = T::NF, kSlots = T::kSlots, kRegs = sizeof(typename T::Acc) / 4, kWaveLds = stream_wave_lds<HD, C>();
+  using T = Math<E, HD, C>;
+  constexpr int ES = sizeof(E), NS = T::NS, NA = T::NA, kSlots = T::kSlots, kRegs = sizeof(typename T::Acc) / 4, kWaveLds = stream_wave_lds<E, HD, C>();
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -159,7 +226,7 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   const int row = p.by_group.quotient(in), head = w.g * p.group + in - row * p.group;
   const RowSight sight = sight_of<SEES>(p, w, row);
 
-  const ItemBase item = item_base<SEES>(p, w);
+  const ItemBase item = item_base<ES, SEES>(p, w);
   // tiles 64 i .. 64 i + 63 of this wavefront's, one per lane: where they are
   TilePlace places;
   auto look_up = [&](int j0) __attribute__((always_inline)) {
@@ -202,8 +269,11 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
 #pragma unroll
     for (int i = 0; i < kRegs; ++i) acc[e][i] = 0.f;
   float m_run = kNoMax, l_run = 0.f;
-  bf16x8 qf[T::NQ], a[NF], pb[T::NB];
-  i16x8 f[NF];
+  typename T::Q qf[T::NQ];
+  typename T::K a[T::NK];
+  typename T::V f[T::NV];
+  typename T::P pb[T::NB];
+  constexpr int kPerP = NS / T::NB;
   float s[NS];
 
   // Requests in order: K(0), V(0), K(1), and then for each tile j K(j+2), V(j+1).  The waits count them.  Loads by the compiler in between (pages)
@@ -212,6 +282,7 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   TilePlace next{};
   auto landed = [&](bool all) __attribute__((always_inline)) {
     if (all) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else if constexpr (T::kFetches == 16) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
     else if constexpr (T::kFetches == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
     wave_lds_sync();
@@ -257,7 +328,7 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
     for (int i = 0; i < NS; ++i) {
       const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], p.scale_log2, -m_run));
       l_loc += e;
-      pb[i >> 3][i & 7] = (__bf16)e;
+      pb[i / kPerP][i % kPerP] = (E)e;   // rounded: bf16
     }
     l_run += l_loc;
   };
@@ -270,9 +341,9 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
     in_issue_order();
     fetch(of_v, true, v_lds);
     in_issue_order();
-    const u32x4* q = reinterpret_cast<const u32x4*>((const char*)p.q + 2 * (w.b * p.q_sb + head * p.q_sh + row * p.q_sr));
+    const u32x4* q = reinterpret_cast<const u32x4*>((const char*)p.q + ES * (w.b * p.q_sb + head * p.q_sh + row * p.q_sr));
 #pragma unroll
-    for (int i = 0; i < T::NQ; ++i) qf[i] = __builtin_bit_cast(bf16x8, q[T::q_piece(i, lane)]);
+    for (int i = 0; i < T::NQ; ++i) qf[i] = __builtin_bit_cast(typename T::Q, q[T::q_piece(i, lane)]);
     // logits of tile j, second product of tile j - 1, softmax of tile j
 #pragma clang loop unroll(disable)
     for (int j = 0; j <= n_mine; ++j) {
@@ -296,13 +367,9 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   }
 
   if (specials)
-    add_specials<SEES>(p, w, sight, 2, 0, n_mine, [&](int j) { return t_begin + j * NW; }, [&](const char* v, bool sees) __attribute__((always_inline)) {
+    add_specials<SEES>(p, w, sight, ES, 0, n_mine, [&](int j) { return t_begin + j * NW; }, [&](const char* v, bool sees) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < kSlots; ++i) {
-        const f32x4 z = special_values(v, T::channel(i, lane), sees);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) acc[C == 32 ? i >> 2 : i][C == 32 ? (i & 3) * 4 + k : k] += z[k];
-      }
+      for (int i = 0; i < kSlots; ++i) T::add(acc, i, special_values<E>(v, T::channel(i, lane), sees));
     });
   const float l_tot = T::over_row(l_run, true);
   // Merge: every wavefront parks its results (slot i of a lane in place i ^ its turn) and its columns' statistics; they then share out the slots, with
@@ -345,10 +412,11 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
     if (w.n_split > 1) {
       *reinterpret_cast<f32x4*>(p.part_o + ((int64_t)w.slot * C + col) * HD + d0) = o4;
     } else {
-      bf16x4 ob;
+      typedef __attribute__((ext_vector_type(4))) E E4;
+      E4 ob;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) ob[r] = (__bf16)(sight.none ? 0.f : o4[r] * inv);
-      *reinterpret_cast<bf16x4*>((__bf16*)p.out + w.b * p.o_sb + head * p.o_sh + row * p.o_sr + d0) = ob;
+      for (int r = 0; r < 4; ++r) ob[r] = (E)(sight.none ? 0.f : o4[r] * inv);
+      *reinterpret_cast<E4*>((E*)p.out + w.b * p.o_sb + head * p.o_sh + row * p.o_sr + d0) = ob;
     }
   }
   if (w.n_split > 1 && wave == 0 && lane < C) {
@@ -357,34 +425,35 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   }
 }
 
-template <int HD, int C, int NW, int SEES>
+template <typename E, int HD, int C, int NW, int SEES>
 hipError_t launch_sees(const PagedAttnParams& p, const PagedPlan& pl, hipStream_t s) {
   static LdsOptIn lds;
-  const auto kernel = attn_paged_stream_kernel<HD, C, NW, SEES>;
-  constexpr int kLds = NW * stream_wave_lds<HD, C>();
+  const auto kernel = attn_paged_stream_kernel<E, HD, C, NW, SEES>;
+  constexpr int kLds = NW * stream_wave_lds<E, HD, C>();
   hipError_t e = lds.ensure(reinterpret_cast<const void*>(kernel), kLds);
   if (e != hipSuccess) return e;
   e = launch(kernel, dim3((unsigned)p.workgroups), dim3(NW * kWave), kLds, s, p);
-  return e != hipSuccess || !pl.splits ? e : launch_paged_merge<__bf16, HD>(p, s);
+  return e != hipSuccess || !pl.splits ? e : launch_paged_merge<E, HD>(p, s);
 }
 
-template <int HD, int C>
-hipError_t launch_cols(const PagedAttnParams& p, const PagedPlan& pl, int sees, hipStream_t s) {
-  if (pl.waves == 8) return sees == kSeeTree ? launch_sees<HD, C, 8, kSeeTree>(p, pl, s) : launch_sees<HD, C, 8, kSeeWindow>(p, pl, s);
-  if (pl.waves != 4) return hipErrorInvalidValue;
-  return sees == kSeeTree ? launch_sees<HD, C, 4, kSeeTree>(p, pl, s) : launch_sees<HD, C, 4, kSeeWindow>(p, pl, s);
+template <typename E, int HD, int C, int NW>
+hipError_t launch_waves(const PagedAttnParams& p, const PagedPlan& pl, int sees, hipStream_t s) {
+  return sees == kSeeTree ? launch_sees<E, HD, C, NW, kSeeTree>(p, pl, s) : launch_sees<E, HD, C, NW, kSeeWindow>(p, pl, s);
 }
 
 template <int HD>
-hipError_t launch_dim(const PagedAttnParams& p, const PagedPlan& pl, int sees, hipStream_t s) {
-  return p.block_cols == 16 ? launch_cols<HD, 16>(p, pl, sees, s) : launch_cols<HD, 32>(p, pl, sees, s);
+hipError_t launch_dim(const PagedAttnParams& p, const PagedPlan& pl, int sees, int dtype, hipStream_t s) {
+  if (dtype != 0) return launch_waves<float, HD, 16, paged_waves_f32(HD)>(p, pl, sees, s);
+  if (p.block_cols == 16) return pl.waves == 4 ? launch_waves<__bf16, HD, 16, 4>(p, pl, sees, s) : launch_waves<__bf16, HD, 16, 8>(p, pl, sees, s);
+  return pl.waves == 4 ? launch_waves<__bf16, HD, 32, 4>(p, pl, sees, s) : launch_waves<__bf16, HD, 32, 8>(p, pl, sees, s);
 }
 
 }  // namespace
 
-hipError_t launch_attn_paged_stream(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s) {
-  if (p.block_cols != 16 && p.block_cols != 32) return hipErrorInvalidValue;
-  return d == 128 ? launch_dim<128>(p, pl, sees, s) : launch_dim<64>(p, pl, sees, s);
+hipError_t launch_attn_paged_stream(const PagedAttnParams& p, const PagedPlan& pl, int sees, int dtype, int d, hipStream_t s) {
+  const bool fits = dtype == 0 ? (p.block_cols == 16 || p.block_cols == 32) && (pl.waves == 4 || pl.waves == 8) : p.block_cols == 16 && pl.waves == paged_waves_f32(d);
+  if (!fits) return hipErrorInvalidValue;
+  return d == 128 ? launch_dim<128>(p, pl, sees, dtype, s) : launch_dim<64>(p, pl, sees, dtype, s);
 }
 
 }  // namespace sdllm

@@ -46,14 +46,13 @@ int32_t fill_cache(const sdllm_paged_shape_t& s, const void* k_pages, const void
   return SDLLM_OK;
 }
 
-enum { kPagedF32 = 0, kPagedStream = 1, kPagedShared = 2 };
-
 // How a call is cut up (paged_tile.h): columns of a workgroup by the kernel, and how many workgroups there are for shares of the tiles.
 int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   const int64_t cols = (int64_t)s.rows * (s.n_q_heads / s.n_kv_heads);
   pl = PagedPlan{};
-  pl.kernel = s.dtype == SDLLM_F32 ? kPagedF32 : cols <= 32 ? kPagedStream : kPagedShared;
-  pl.block_cols = pl.kernel == kPagedF32 ? kGeneralRowsF32 : pl.kernel == kPagedStream ? (cols <= 16 ? 16 : 32) : cols <= 128 ? 128 : 256;
+  const bool f32 = s.dtype == SDLLM_F32;
+  pl.shared = !f32 && cols > 32;
+  pl.block_cols = f32 || cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 128 ? 128 : 256;
   // columns, blocks and threads of a launch (the merge's too) are counted in 32 bits
   if (cols > INT32_MAX - 256) return SDLLM_ERR_UNSUPPORTED;
   pl.max_blocks = (int)((cols + pl.block_cols - 1) / pl.block_cols);
@@ -69,11 +68,11 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
     tiles = std::min<int64_t>(tiles, ((int64_t)s.window_left + s.window_right + pl.block_cols) / kTileKeys + 2 + std::min(s.sinks, capacity) / kTileKeys);
   // With few items a workgroup has the eight wavefronts that a CU's LDS has room for, with many of them two of four wavefronts share it, one starting or
   // merging while the other streams.
-  pl.waves = pl.kernel == kPagedStream && items > 64 ? 4 : 8;
-  const int64_t at_once = pl.waves == 4 ? 2 * kNumCUs : kNumCUs;
-  pl.least_tiles = pl.kernel == kPagedStream ? 6 * pl.waves : 16;
+  pl.waves = f32 ? paged_waves_f32(s.head_dim) : !pl.shared && items > 64 ? 4 : 8;
+  const int64_t at_once = !f32 && pl.waves == 4 ? 2 * kNumCUs : kNumCUs;
+  pl.least_tiles = f32 ? 2 * pl.waves : pl.shared ? 16 : 6 * pl.waves;
   // A second round of workgroups that share columns' keys costs more than uneven items do
-  pl.splits = items <= (pl.kernel == kPagedShared ? 160 : 2 * at_once) && tiles > pl.least_tiles;
+  pl.splits = items <= (pl.shared ? 160 : 2 * at_once) && tiles > pl.least_tiles;
   pl.workgroups = pl.splits ? (int)std::max<int64_t>(at_once, 2 * items) : (int)items;
   while (tiles >> pl.tile_shift >= 1 << 20) ++pl.tile_shift;   // items <= 1024
   return SDLLM_OK;
@@ -132,15 +131,13 @@ int32_t run_paged(const sdllm_paged_shape_t* shape, bool tree, const void* q, co
   p.chunk = std::min(pl.max_blocks, 4);
   p.by_chunk = Divisor((uint32_t)p.chunk);
   p.by_group = Divisor((uint32_t)p.group); p.by_blocks = Divisor((uint32_t)p.max_blocks); p.by_hkv = Divisor((uint32_t)p.hkv);
-  return launch_attn_paged(p, pl, tree ? kSeeTree : kSeeWindow, s.head_dim, (hipStream_t)stream) == hipSuccess ? SDLLM_OK : SDLLM_ERR_HIP;
+  return launch_attn_paged(p, pl, tree ? kSeeTree : kSeeWindow, s.dtype, s.head_dim, (hipStream_t)stream) == hipSuccess ? SDLLM_OK : SDLLM_ERR_HIP;
 }
 
 }  // namespace
 
-hipError_t sdllm::launch_attn_paged(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s) {
-  return pl.kernel == kPagedF32      ? launch_attn_paged_f32(p, pl, sees, d, s)
-         : pl.kernel == kPagedStream ? launch_attn_paged_stream(p, pl, sees, d, s)
-                                     : launch_attn_paged_shared(p, pl, sees, d, s);
+hipError_t sdllm::launch_attn_paged(const PagedAttnParams& p, const PagedPlan& pl, int sees, int dtype, int d, hipStream_t s) {
+  return pl.shared ? launch_attn_paged_shared(p, pl, sees, d, s) : launch_attn_paged_stream(p, pl, sees, dtype, d, s);
 }
 
 extern "C" {

@@ -1,4 +1,4 @@
-// What the bf16 kernels of the paged cache's attention share: masks, the softmax reference, values that are no numbers, and where a tile's rows are.
+// What the kernels of the paged cache's attention share about values and places: masks, the softmax reference, values that are no numbers, and where a tile's rows are.
 #pragma once
 
 #include "attn_tile_math.h"
@@ -29,7 +29,22 @@ __device__ __forceinline__ void move_reference_to(float m_loc, float& m_ref, flo
   }
 }
 
-// Takes values that are no numbers out of a masked tile's operands (paged_tile.h), two values a word; true for all lanes if there are any.
+// Takes values that are no numbers out of a masked tile's operands (paged_tile.h); true for all lanes if there are any.  bf16: two values a word.
+template <int N>
+__device__ __forceinline__ bool take_specials(f32x4 (&f)[N]) {
+  auto special = [](float v) { return ((__builtin_bit_cast(uint32_t, v) & 0x7f800000u) + 0x00800000u) & 0x80000000u; };   // bit 31: the exponent is all ones
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) any |= special(f[i][j]);
+  if (__ballot(any != 0) == 0) return false;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[i][j] = special(f[i][j]) ? 0.f : f[i][j];
+  return true;
+}
 template <int N>
 __device__ __forceinline__ bool take_specials(i16x8 (&f)[N]) {
   // bits 15 and 31: the exponents that are all ones
@@ -53,35 +68,36 @@ __device__ __forceinline__ bool take_specials(i16x8 (&f)[N]) {
 }
 
 // add_specials' share of four channels of a row of V
+template <typename E>
 __device__ __forceinline__ f32x4 special_values(const char* v, int channel, bool sees) {
-  const bf16x4 u = *reinterpret_cast<const bf16x4*>(v + 2 * channel);
+  const E* u = reinterpret_cast<const E*>(v) + channel;
   f32x4 z;
 #pragma unroll
   for (int k = 0; k < 4; ++k) z[k] = sees && !(fabsf((float)u[k]) < INFINITY) ? (float)u[k] : 0.f;
   return z;
 }
 
-// Where the rows of an item are (bf16), in bytes: its pages' and its own (kSeeTree) rows of the KV head
+// Where the rows of an item are, in bytes (ES an element): its pages' and its own (kSeeTree) rows of the KV head
 struct ItemBase {
   const char *k, *v, *k_own, *v_own;
   int64_t page;
   uint32_t stride, stride_own, row_mask;
 };
-template <int SEES>
+template <int ES, int SEES>
 __device__ __forceinline__ ItemBase item_base(const PagedAttnParams& p, const PagedItem& w) {
   ItemBase r{};
   const PagedCache& c = p.cache;
-  const int64_t at = 2 * (w.g * c.sh);
+  const int64_t at = ES * (w.g * c.sh);
   r.k = (const char*)p.k_pages + at;
   r.v = (const char*)p.v_pages + at;
-  r.page = 2 * c.sp;
-  r.stride = (uint32_t)(c.sr * 2);
+  r.page = ES * c.sp;
+  r.stride = (uint32_t)(c.sr * ES);
   r.row_mask = (1u << c.page_shift) - 1;
   if (SEES == kSeeTree) {
-    const int64_t own = 2 * (w.b * p.blk_sb + w.g * p.blk_sh);
+    const int64_t own = ES * (w.b * p.blk_sb + w.g * p.blk_sh);
     r.k_own = (const char*)p.k_blk + own;
     r.v_own = (const char*)p.v_blk + own;
-    r.stride_own = (uint32_t)(p.blk_sr * 2);
+    r.stride_own = (uint32_t)(p.blk_sr * ES);
   }
   return r;
 }

@@ -353,11 +353,11 @@ hipError_t launch_unpack(const PackParams& p, int dtype, int d, hipStream_t s);
 hipError_t launch_attn_packed(const PackedAttnParams& p, int dtype, int d, hipStream_t s);
 hipError_t launch_qk_norm_rope(const QkParams& p, int dtype, int d, hipStream_t s);
 hipError_t launch_append_paged(const AppendParams& p, int dtype, int d, hipStream_t s);
-// how a call is cut up; pl of a launch or of the host's question
-struct PagedPlan { int kernel, block_cols, waves, max_blocks, workgroups, least_tiles, tile_shift; bool splits; };
-hipError_t launch_attn_paged(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
-hipError_t launch_attn_paged_f32(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
+// how a call is cut up
+struct PagedPlan { bool shared; int block_cols, waves, max_blocks, workgroups, least_tiles, tile_shift; bool splits; };
+constexpr int paged_waves_f32(int d) { return d == 128 ? 4 : 8; }   // that a CU's LDS has room for
+hipError_t launch_attn_paged(const PagedAttnParams& p, const PagedPlan& pl, int sees, int dtype, int d, hipStream_t s);
 hipError_t launch_attn_paged_shared(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
-hipError_t launch_attn_paged_stream(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
+hipError_t launch_attn_paged_stream(const PagedAttnParams& p, const PagedPlan& pl, int sees, int dtype, int d, hipStream_t s);
 
 }  // namespace sdllm
