@@ -172,7 +172,7 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
     // The 64 tiles at hand change before the K of a step that begins with the next; V of the step before has been asked for by then.
     auto turn_page = [&](int step) __attribute__((always_inline)) {
       const int n = step * KS * KT;
-      if ((n & 63) == 0 && n < n_tiles) look_up(n);
+      if (n > 0 && (n & 63) == 0 && n < n_tiles) look_up(n);
     };
     static_assert(64 % (KS * KT) == 0, "a step's tiles are among the same 64");
 
@@ -240,27 +240,23 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
       l_run += l;
     };
 
-    // Requests are counted, in the order K(0), V(0), K(1), V(1), K(2), ..., V(N-1), K(N) and then V(t+N), K(t+N+1) for t = 0, 1, ...  Loads by the compiler
-    // (pages, masks, query rows) make a wait longer, never shorter.
+    // Requests are counted, in the order K(0), V(0), K(1), V(1), ..., V(N-1), K(N) and then V(t+N), K(t+N+1) for t = 0, 1, ...  Loads by the compiler
+    // (pages) make a wait longer, never shorter; query rows, masks and the first pages are waited for before the first request.
     look_up(0);
-    fetch_k(0, 0);
-    fetch_v(0, 0);
-    turn_page(1);
-    fetch_k(1, kStepK);
-    in_issue_order();
 #pragma unroll
     for (int i = 0; i < NP; ++i) asm volatile("" : "+v"(qf[i]));
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    bare_barrier();
 #pragma unroll
-    for (int j = 1; j < N; ++j) {
-      if (j > 1) {
-        turn_page(j);
-        fetch_k(j, j * kStepK);
-      }
+    for (int j = 0; j < N; ++j) {
+      turn_page(j);
+      fetch_k(j, j * kStepK);
+      in_issue_order();
       fetch_v(j, j * kStepV);
+      in_issue_order();
     }
-    in_issue_order();
+    // V(1), K(2), ..., V(N-1) may still fly
+    if (KS == 1) asm volatile("s_waitcnt vmcnt(7)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
+    bare_barrier();
 #pragma unroll
     for (int i = 0; i < 8; ++i) a[i] = S::k_frag(k_at, i);
 #pragma unroll
@@ -359,12 +355,33 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
   };
   if constexpr (KS == 1) {
     const float inv = 1.f / l_tot;
-    if (there) {
+    if (w.n_split > 1) {
+      if (there) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e)
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4)
+            put(out_col0(e, i4, half), f32x4{acc[e][i4 * 4], acc[e][i4 * 4 + 1], acc[e][i4 * 4 + 2], acc[e][i4 * 4 + 3]}, inv);
+      }
+    } else {
+      // Four channels of a lane and the four after them of the lane 32 on, twice: exchanged, so that each has eight in a row to write
 #pragma unroll
       for (int e = 0; e < NE; ++e)
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4)
-          put(out_col0(e, i4, half), f32x4{acc[e][i4 * 4], acc[e][i4 * 4 + 1], acc[e][i4 * 4 + 2], acc[e][i4 * 4 + 3]}, inv);
+        for (int i4 = 0; i4 < 4; i4 += 2) {
+          bf16x4 ab[2];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) ab[k >> 2][k & 3] = (__bf16)(none ? 0.f : acc[e][i4 * 4 + k] * inv);
+          u32x2 x = __builtin_bit_cast(u32x2, ab[0]), y = __builtin_bit_cast(u32x2, ab[1]);
+          u32x4 o;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const auto z = __builtin_amdgcn_permlane32_swap(x[k], y[k], false, false);
+            o[k] = z[0];
+            o[2 + k] = z[1];
+          }
+          if (there) *reinterpret_cast<u32x4*>(out + 32 * e + 8 * (i4 + half)) = o;
+        }
     }
   } else {
     // merge of the key groups of each block of columns
