@@ -51,12 +51,14 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   const int64_t cols = (int64_t)s.rows * (s.n_q_heads / s.n_kv_heads);
   pl = PagedPlan{};
   const bool f32 = s.dtype == SDLLM_F32;
-  pl.shared = !f32 && cols > 32;
-  pl.block_cols = f32 || cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 128 ? 128 : 256;
+  const int64_t heads = (int64_t)s.batch * s.n_kv_heads;
+  // Up to 64 columns two blocks that read the same tiles, one of them from L2, are ahead of waves that share them (8 trees of 16 rows x 32/8 heads x 4096 rows
+  // 33.7 us, shared 42.5), up to 128 where there are few heads (one tree of 32 rows x 32/8 heads x 8192 rows 21.5, shared 27.2; 8 trees 46.0, 44.7).
+  pl.shared = !f32 && cols > (heads <= 16 ? 128 : 64);
+  pl.block_cols = f32 || cols <= 16 ? 16 : !pl.shared ? 32 : cols <= 128 ? 128 : 256;
   // columns, blocks and threads of a launch (the merge's too) are counted in 32 bits
   if (cols > INT32_MAX - 256) return SDLLM_ERR_UNSUPPORTED;
   pl.max_blocks = (int)((cols + pl.block_cols - 1) / pl.block_cols);
-  const int64_t heads = (int64_t)s.batch * s.n_kv_heads;
   if (heads > INT32_MAX) return SDLLM_ERR_UNSUPPORTED;
   const int64_t items = heads * pl.max_blocks;
   if (items > UINT32_MAX / (kGeneralMaxWaves * kWave)) return SDLLM_ERR_UNSUPPORTED;
@@ -70,7 +72,7 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   // merging while the other streams.
   pl.waves = f32 ? paged_waves_f32(s.head_dim) : !pl.shared && items > 64 ? 4 : 8;
   const int64_t at_once = !f32 && pl.waves == 4 ? 2 * kNumCUs : kNumCUs;
-  pl.least_tiles = f32 ? 2 * pl.waves : pl.shared ? 16 : 6 * pl.waves;
+  pl.least_tiles = f32 ? 2 * pl.waves : pl.shared ? 8 : 6 * pl.waves;
   // A second round of workgroups that share columns' keys costs more than uneven items do
   pl.splits = items <= (pl.shared ? 160 : 2 * at_once) && tiles > pl.least_tiles;
   pl.workgroups = pl.splits ? (int)std::max<int64_t>(at_once, 2 * items) : (int)items;

@@ -119,7 +119,7 @@ __device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, Pa
     w.n_split = 1;
     w.slot = 0;
     locate_item<SEES>(p, w);
-    w.past_caches = (int64_t)gridDim.x * w.tiles >= p.caches_tiles;   // a guess: as if all items were like this one
+    w.past_caches = p.max_blocks == 1 && (int64_t)gridDim.x * w.tiles >= p.caches_tiles;   // a guess: as if all items were like this one
     return true;
   }
   struct Seq { int length, count, blocks, tiles; };
@@ -157,7 +157,7 @@ __device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, Pa
     used = used_at(share);
   }
   if ((int)blockIdx.x >= used) return false;
-  w.past_caches = (int64_t)tiles << p.tile_shift >= p.caches_tiles;
+  w.past_caches = p.max_blocks == 1 && (int64_t)tiles << p.tile_shift >= p.caches_tiles;
   const int id = chunked_id(p, blockIdx.x, used);
   int before = 0;
   for (int b0 = 0; b0 < p.batch; b0 += kWave) {
