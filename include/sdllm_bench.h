@@ -66,6 +66,17 @@ typedef struct sdllm_packed_plan {
 /* How sdllm_sparse_attn_packed of this shape over n_cached rows, or state 2 of sdllm_block_step_packed, is launched.  Host only. */
 int32_t sdllm_packed_plan(const sdllm_shape_t* shape, int32_t n_cached, sdllm_packed_plan_t* plan);
 
+typedef struct sdllm_paged_plan {
+  int32_t shared;      /* 1: the waves of a workgroup share tiles; 0: each streams its own */
+  int32_t block_cols;  /* query rows x heads of a KV head's group that a workgroup takes */
+  int32_t waves;       /* per workgroup */
+  int32_t workgroups;  /* of the launch: as many as there are blocks of columns, or as many as the blocks' shares of the tiles may be */
+  int32_t least_tiles; /* 32-key tiles below which a share is not cut; 0: no block is cut, and there is no second launch */
+} sdllm_paged_plan_t;
+
+/* How SDLLM_OP_TREE_ATTN_PAGED or SDLLM_OP_WINDOW_ATTN_PAGED of this shape is launched; what a workgroup does is found from the lengths.  Host only. */
+int32_t sdllm_paged_plan(const sdllm_paged_shape_t* shape, int32_t op, sdllm_paged_plan_t* plan);
+
 /* SDLLM_CALL_DENSE on SDLLM_KERNEL_DENSE: *groups is the key groups of the launch that the workgroups of a last, small round are, 0 for a
  * call (or a shape) without such a launch.  Host only. */
 int32_t sdllm_dense_tail_groups(const sdllm_shape_t* shape, int32_t* groups);

@@ -37,7 +37,7 @@ EXPORTED = ("sdllm_error_string", "sdllm_version", "sdllm_retained_count", "sdll
             "sdllm_compact_kv_packed", "sdllm_unpack_kv", "sdllm_sparse_attn_packed", "sdllm_block_step_packed",
             "sdllm_qk_norm_rope", "sdllm_paged_workspace_bytes", "sdllm_append_paged", "sdllm_tree_attn_paged", "sdllm_window_attn_paged",
             "sdllm_stream_read_probe",
-            "sdllm_launch_plan", "sdllm_packed_plan", "sdllm_burst_splits", "sdllm_dense_tail_groups",
+            "sdllm_launch_plan", "sdllm_packed_plan", "sdllm_paged_plan", "sdllm_burst_splits", "sdllm_dense_tail_groups",
             "sdllm_column_kernel")
 
 # constants of include/sdllm_bench.h
@@ -86,6 +86,11 @@ class sdllm_launch_plan_t(ctypes.Structure):
 
 class sdllm_packed_plan_t(ctypes.Structure):
     _fields_ = [("key_splits", ctypes.c_int32), ("waves", ctypes.c_int32), ("rounds", ctypes.c_int32), ("past_caches", ctypes.c_int32)]
+
+
+class sdllm_paged_plan_t(ctypes.Structure):
+    _fields_ = [("shared", ctypes.c_int32), ("block_cols", ctypes.c_int32), ("waves", ctypes.c_int32), ("workgroups", ctypes.c_int32),
+                ("least_tiles", ctypes.c_int32)]
 
 
 class SdllmError(RuntimeError):
@@ -158,6 +163,8 @@ def load() -> ctypes.CDLL:
     lib.sdllm_launch_plan.argtypes = [shp, i32, i32, ctypes.POINTER(sdllm_launch_plan_t)]
     lib.sdllm_packed_plan.restype = i32
     lib.sdllm_packed_plan.argtypes = [shp, i32, ctypes.POINTER(sdllm_packed_plan_t)]
+    lib.sdllm_paged_plan.restype = i32
+    lib.sdllm_paged_plan.argtypes = [paged, i32, ctypes.POINTER(sdllm_paged_plan_t)]
     lib.sdllm_burst_splits.restype = i32
     lib.sdllm_burst_splits.argtypes = [shp, i32, i32, i32p]
     lib.sdllm_dense_tail_groups.restype = i32
@@ -487,6 +494,12 @@ def sdllm_launch_plan(shape: sdllm_shape_t, call: int, n_cached: int = 0) -> sdl
 def sdllm_packed_plan(shape: sdllm_shape_t, n_cached: int) -> sdllm_packed_plan_t:
     plan = sdllm_packed_plan_t()
     _check(load().sdllm_packed_plan(ctypes.byref(shape), n_cached, ctypes.byref(plan)), "sdllm_packed_plan")
+    return plan
+
+
+def sdllm_paged_plan(shape: sdllm_paged_shape_t, op: int) -> sdllm_paged_plan_t:
+    plan = sdllm_paged_plan_t()
+    _check(load().sdllm_paged_plan(ctypes.byref(shape), op, ctypes.byref(plan)), "sdllm_paged_plan")
     return plan
 
 

@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "api_checks.h"
+#include "sdllm_bench.h"
 #include "sdllm_internal.h"
 
 using namespace sdllm;
@@ -89,6 +90,14 @@ PagedBytes paged_bytes(const sdllm_paged_shape_t& s, const PagedPlan& pl) {
 
 int32_t check_op(const sdllm_paged_shape_t& s, bool tree) { return tree && s.rows > 64 ? SDLLM_ERR_UNSUPPORTED : SDLLM_OK; }
 
+int32_t plan_of_op(const sdllm_paged_shape_t* s, int32_t op, PagedPlan& pl) {
+  const bool tree = op == SDLLM_OP_TREE_ATTN_PAGED;
+  if (!tree && op != SDLLM_OP_WINDOW_ATTN_PAGED) return SDLLM_ERR_INVALID_ARG;
+  int32_t st = check_paged(s);
+  if (st == SDLLM_OK) st = check_op(*s, tree);
+  return st == SDLLM_OK ? plan_paged(*s, tree, pl) : st;
+}
+
 int32_t run_paged(const sdllm_paged_shape_t* shape, bool tree, const void* q, const void* k_pages, const void* v_pages, const int32_t* table,
                   const int32_t* lengths, const int32_t* row_counts, const void* k_blk, const void* v_blk, const uint64_t* mask, void* out, void* ws,
                   size_t ws_bytes, void* stream) {
@@ -144,14 +153,20 @@ hipError_t sdllm::launch_attn_paged(const PagedAttnParams& p, const PagedPlan& p
 
 extern "C" {
 
-int32_t sdllm_paged_workspace_bytes(const sdllm_paged_shape_t* shape, int32_t op, size_t* bytes) {
-  int32_t st = check_paged(shape);
-  if (st != SDLLM_OK) return st;
-  if (!bytes || (op != SDLLM_OP_TREE_ATTN_PAGED && op != SDLLM_OP_WINDOW_ATTN_PAGED)) return SDLLM_ERR_INVALID_ARG;
-  const bool tree = op == SDLLM_OP_TREE_ATTN_PAGED;
-  if ((st = check_op(*shape, tree)) != SDLLM_OK) return st;
+int32_t sdllm_paged_plan(const sdllm_paged_shape_t* shape, int32_t op, sdllm_paged_plan_t* plan) {
   PagedPlan pl;
-  if ((st = plan_paged(*shape, tree, pl)) != SDLLM_OK) return st;
+  const int32_t st = plan_of_op(shape, op, pl);
+  if (st != SDLLM_OK) return st;
+  if (!plan) return SDLLM_ERR_INVALID_ARG;
+  *plan = sdllm_paged_plan_t{pl.shared, pl.block_cols, pl.waves, pl.workgroups, pl.splits ? pl.least_tiles : 0};
+  return SDLLM_OK;
+}
+
+int32_t sdllm_paged_workspace_bytes(const sdllm_paged_shape_t* shape, int32_t op, size_t* bytes) {
+  PagedPlan pl;
+  const int32_t st = plan_of_op(shape, op, pl);
+  if (st != SDLLM_OK) return st;
+  if (!bytes) return SDLLM_ERR_INVALID_ARG;
   *bytes = std::max(paged_bytes(*shape, pl).all(), kAlign);   // never zero, so callers can always allocate
   return SDLLM_OK;
 }
