@@ -1,21 +1,21 @@
-// Merge of the splits of the paged cache's attention: what the workgroups of an item left, folded with the usual rescaling, as a launch of its own.
+// Merge of the shares of the paged cache's attention: what the workgroups of an item left, folded with the usual rescaling, as a launch of its own.
 // An item's first workgroup says where its partials are and how many (item_at).  Bound by round trips: the item's place, then everything else
-// of up to eight splits at once; with many splits eight lanes take every eighth each.
+// of several shares at once, with many shares by eight lanes that take every eighth each.
 #pragma once
 
 #include "attn_merge.h"
-#include "paged_tile.h"
+#include "paged_math.h"
 
 namespace sdllm {
 
 constexpr int kPagedMergeThreads = 256;
 
-// TPI adjacent lanes fold the splits of one column's four channels; blockIdx.x is the item, blockIdx.y a part of its columns.
-template <typename T, int D, int TPI>
+// TPI adjacent lanes fold the shares of four channels of a column, NB shares at a time; blockIdx.x is the item, blockIdx.y a part of its results.
+template <typename E, int HD, int C, int TPI, int NB>
 __global__ __launch_bounds__(kPagedMergeThreads) void attn_paged_merge_kernel(const PagedAttnParams p) {
-  constexpr int kPer = D / 4 * TPI;     // threads of a column
-  const int item = blockIdx.x, tid = blockIdx.y * kPagedMergeThreads + threadIdx.x;
-  const int col = tid / kPer, sub = tid % TPI, c4 = tid % kPer / TPI * 4;
+  using M = Math<E, HD, C>;
+  const int item = blockIdx.x, tid = blockIdx.y * kPagedMergeThreads + threadIdx.x, sub = tid % TPI;
+  const int at = tid / TPI, lane = at % kWave, i = at / kWave % M::kSlots, cols = at / (kWave * M::kSlots), col = cols * C + lane % C;
   const int head = p.by_blocks.quotient(item), blk = item - head * p.max_blocks;
   const int b = p.by_hkv.quotient(head), g = head - b * p.hkv;
   const int column = blk * p.block_cols + col;
@@ -23,9 +23,9 @@ __global__ __launch_bounds__(kPagedMergeThreads) void attn_paged_merge_kernel(co
   // an item that is not there has left nothing, not even its place
   if (column >= p.cache.count(b) * p.group || col >= p.block_cols || n_split < 2) return;
   const float* ml = p.part_ml + (int64_t)slot * 2 * p.block_cols + col;
-  const float* po = p.part_o + ((int64_t)slot * p.block_cols + col) * D + c4;
+  const mf32x4* po = reinterpret_cast<const mf32x4*>(partial_slot<M>(p, slot, cols, i, lane));
+  const int64_t next = (int64_t)p.block_cols * HD / 4;
   RowPiece r;
-  constexpr int NB = 8;
   for (int s0 = sub; s0 < n_split; s0 += NB * TPI) {
     float m_s[NB], l_s[NB];
     mf32x4 o_s[NB];
@@ -34,7 +34,7 @@ __global__ __launch_bounds__(kPagedMergeThreads) void attn_paged_merge_kernel(co
       const int64_t s = min(s0 + u * TPI, n_split - 1);   // past the end: left out below
       m_s[u] = ml[s * 2 * p.block_cols];
       l_s[u] = ml[s * 2 * p.block_cols + p.block_cols];
-      o_s[u] = *reinterpret_cast<const mf32x4*>(po + s * p.block_cols * D);
+      o_s[u] = po[s * next];
     }
 #pragma unroll
     for (int u = 0; u < NB; ++u) {
@@ -56,27 +56,26 @@ __global__ __launch_bounds__(kPagedMergeThreads) void attn_paged_merge_kernel(co
   }
   if (sub != 0) return;
   const int row = p.by_group.quotient(column), h = g * p.group + column - row * p.group;
-  T* out = (T*)p.out + b * p.o_sb + h * p.o_sh + row * p.o_sr + c4;
   if (r.m == -INFINITY) {   // the row sees nothing
     r.l = 1.f;
     r.o = mf32x4{0.f, 0.f, 0.f, 0.f};
   }
-  store_piece<T>(r, out);
+  store_piece<E>(r, (E*)p.out + b * p.o_sb + h * p.o_sh + row * p.o_sr + M::channel(i, lane));
 }
 
-template <typename T, int D, int TPI>
+template <typename E, int HD, int C, int TPI, int NB>
 hipError_t launch_paged_merge_by(const PagedAttnParams& p, int most_cols, hipStream_t s) {
-  const int items = p.batch * p.hkv * p.max_blocks, cols = most_cols < p.block_cols ? most_cols : p.block_cols;
-  const dim3 grid((unsigned)items, (unsigned)((cols * (D / 4) * TPI + kPagedMergeThreads - 1) / kPagedMergeThreads));
-  return launch(attn_paged_merge_kernel<T, D, TPI>, grid, dim3(kPagedMergeThreads), 0, s, p);
+  const int items = p.batch * p.hkv * p.max_blocks, blocks = (most_cols + C - 1) / C;
+  const dim3 grid((unsigned)items, (unsigned)(blocks * C * (HD / 4) * TPI / kPagedMergeThreads));
+  return launch(attn_paged_merge_kernel<E, HD, C, TPI, NB>, grid, dim3(kPagedMergeThreads), 0, s, p);
 }
 
-template <typename T, int D>
+template <typename E, int HD, int C>
 hipError_t launch_paged_merge(const PagedAttnParams& p, hipStream_t s) {
   const int64_t cols = (int64_t)p.cache.rows * p.group;
   const int most_cols = cols < p.block_cols ? (int)cols : p.block_cols;
   const int items = p.batch * p.hkv * p.max_blocks;
-  return p.workgroups / items >= 16 ? launch_paged_merge_by<T, D, 8>(p, most_cols, s) : launch_paged_merge_by<T, D, 1>(p, most_cols, s);
+  return p.workgroups / items >= 16 ? launch_paged_merge_by<E, HD, C, 8, 8>(p, most_cols, s) : launch_paged_merge_by<E, HD, C, 1, 8>(p, most_cols, s);
 }
 
 }  // namespace sdllm

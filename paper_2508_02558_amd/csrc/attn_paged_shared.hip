@@ -10,7 +10,6 @@
 #include <type_traits>
 
 #include "attn_paged_merge.h"
-#include "paged_place.h"
 
 namespace sdllm {
 
@@ -339,30 +338,14 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
   asm volatile("" : "+v"(again));   // worked out again rather than kept
   const auto [column, row, head] = column_of(again);
   const bool there = column < w.cols, none = sight_of<SEES>(p, w, row).none;
-  float* part_o = p.part_o + ((int64_t)w.slot * kCols + rb * 32 + col) * HD;
   float* part_ml = p.part_ml + (int64_t)w.slot * 2 * kCols + rb * 32 + col;
   __bf16* out = (__bf16*)p.out + w.b * p.o_sb + head * p.o_sh + row * p.o_sr;
-  // four channels from d0 on
-  auto put = [&](int d0, f32x4 o4, float inv) __attribute__((always_inline)) {
-    if (w.n_split > 1) {
-      *reinterpret_cast<f32x4*>(part_o + d0) = o4;
-    } else {
-      bf16x4 ob;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) ob[r] = (__bf16)(none ? 0.f : o4[r] * inv);
-      *reinterpret_cast<bf16x4*>(out + d0) = ob;
-    }
-  };
+  using M = Math<__bf16, HD, 32>;   // results lie as there
   if constexpr (KS == 1) {
     const float inv = 1.f / l_tot;
     if (w.n_split > 1) {
-      if (there) {
 #pragma unroll
-        for (int e = 0; e < NE; ++e)
-#pragma unroll
-          for (int i4 = 0; i4 < 4; ++i4)
-            put(out_col0(e, i4, half), f32x4{acc[e][i4 * 4], acc[e][i4 * 4 + 1], acc[e][i4 * 4 + 2], acc[e][i4 * 4 + 3]}, inv);
-      }
+      for (int i = 0; i < M::kSlots; ++i) *partial_slot<M>(p, w.slot, rb, i, lane) = M::slot(acc, i);
     } else {
       // Four channels of a lane and the four after them of the lane 32 on, twice: exchanged, so that each has eight in a row to write
 #pragma unroll
@@ -416,14 +399,19 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
     }
     m_run = m_tot;
     const float inv = 1.f / l_tot;
-    if (there) {
 #pragma unroll
-      for (int j = 0; j < NE * 4 / KS; ++j) {
-        const int i = kg * (NE * 4 / KS) + j;
-        f32x4 o4 = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < NE * 4 / KS; ++j) {
+      const int i = kg * (NE * 4 / KS) + j;
+      f32x4 o4 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < KS; ++k) o4 += *reinterpret_cast<const f32x4*>(parked(k) + lane * kLane + i * 16) * f_w[k];
-        put(out_col0(i >> 2, i & 3, half), o4, inv);
+      for (int k = 0; k < KS; ++k) o4 += *reinterpret_cast<const f32x4*>(parked(k) + lane * kLane + i * 16) * f_w[k];
+      if (w.n_split > 1) {
+        *partial_slot<M>(p, w.slot, rb, i, lane) = o4;
+      } else if (there) {
+        bf16x4 ob;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) ob[r] = (__bf16)(none ? 0.f : o4[r] * inv);
+        *reinterpret_cast<bf16x4*>(out + M::channel(i, lane)) = ob;
       }
     }
   }
@@ -442,7 +430,7 @@ hipError_t launch_sees(const PagedAttnParams& p, const PagedPlan& pl, hipStream_
   if (e != hipSuccess) return e;
   if (p.block_cols != 256 / KS) return hipErrorInvalidValue;
   e = launch(kernel, dim3((unsigned)p.workgroups), dim3(512), kLds, s, p);
-  return e != hipSuccess || !pl.splits ? e : launch_paged_merge<__bf16, HD>(p, s);
+  return e != hipSuccess || !pl.splits ? e : launch_paged_merge<__bf16, HD, 32>(p, s);
 }
 
 template <int HD>

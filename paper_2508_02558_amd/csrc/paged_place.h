@@ -47,16 +47,17 @@ __device__ __forceinline__ bool take_specials(f32x4 (&f)[N]) {
 }
 template <int N>
 __device__ __forceinline__ bool take_specials(i16x8 (&f)[N]) {
+  typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
   // bits 15 and 31: the exponents that are all ones
   auto special = [](uint32_t v) { return ((v & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };
-  uint32_t any = 0;
+  u16x2 most = {0, 0};   // of the magnitudes
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const u32x4 v = __builtin_bit_cast(u32x4, f[i]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) any |= special(v[j]);
+    for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, v[j] & 0x7fff7fffu));
   }
-  if (__ballot(any != 0) == 0) return false;
+  if (__ballot(special(__builtin_bit_cast(uint32_t, most)) != 0) == 0) return false;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     u32x4 v = __builtin_bit_cast(u32x4, f[i]);

@@ -243,20 +243,14 @@ __device__ __forceinline__ RowSight sight_of(const PagedAttnParams& p, const Pag
   return r;
 }
 
-// Bits [a, b) of 32, for any a and b
-__device__ __forceinline__ uint32_t bits_between(int a, int b) {
-  a = min(max(a, 0), 32);
-  b = min(max(b, 0), 32);
-  const uint32_t below_b = b == 32 ? ~0u : (1u << b) - 1, below_a = a == 32 ? ~0u : (1u << a) - 1;
-  return below_b & ~below_a;
-}
+// Bits [0, n) of 32, for any n
+__device__ __forceinline__ uint32_t bits_below(int n) { return (uint32_t)(0xffffffffull >> (32 - min(max(n, 0), 32))); }
 
 // Bit r: the row sees key r of the tile
 template <int SEES>
 __device__ __forceinline__ uint32_t seen_bits(const PagedAttnParams& p, const PagedTile& x, const RowSight& r) {
-  if (SEES == kSeeTree) return x.own ? (uint32_t)(r.bits >> x.at) : bits_between(0, x.hi);
-  const uint32_t upto = bits_between(0, r.last + 1 - x.at);
-  return upto & (bits_between(r.first - x.at, 32) | bits_between(0, p.sinks - x.at));
+  if (SEES == kSeeTree) return x.own ? (uint32_t)(r.bits >> x.at) : bits_below(x.hi);
+  return bits_below(r.last + 1 - x.at) & (~bits_below(r.first - x.at) | bits_below(p.sinks - x.at));
 }
 
 // The page that holds a row, one of the pool's in any case

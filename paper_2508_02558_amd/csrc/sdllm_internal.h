@@ -337,7 +337,7 @@ struct PagedAttnParams {
   // plan (plan_paged): what a workgroup takes is found on the device from the lengths
   int32_t block_cols, max_blocks;     // query columns of a workgroup; blocks of them that a KV head has at most
   int32_t workgroups, least_tiles;    // of the launch; 32-key tiles below which a workgroup's share is not cut
-  float* part_o;                      // [workgroups][block_cols][d]; null: nothing is split, workgroups are the items
+  float* part_o;                      // [workgroups][block_cols x d] (paged_math.h); null: nothing is split, workgroups are the items
   float* part_ml;                     // [workgroups][2][block_cols]
   int32_t* item_at;                   // [batch x hkv x max_blocks][2]: first of an item's workgroups in part_*, how many
   int32_t tile_shift;                 // in units of 2^tile_shift the tiles of all items add up in 32 bits
