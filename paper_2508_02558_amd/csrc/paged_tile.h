@@ -35,14 +35,6 @@ __device__ __forceinline__ int chunked_id(const PagedAttnParams& p, int dealt, i
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
-// a / b rounded up, of 0 <= a <= 2^24 + 64 or a ratio below 2^21, and 1 <= b, both below 2^31: the quotient by floats is off by one at most
-__device__ __forceinline__ int ceil_ratio(int a, int b) {
-  int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b));
-  const int64_t r = (int64_t)a - (int64_t)q * b;
-  q += r >= b ? 1 : r < 0 ? -1 : 0;
-  return q + ((int64_t)q * b < a ? 1 : 0);
-}
-
 // Sum of x over the lanes up to this one, in registers (shuffles go through LDS)
 __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1, 2, 4, 8: within rows of 16
@@ -140,29 +132,31 @@ __device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, Pa
   };
   const int items = over_all([](const Seq&, int heads) { return heads; });
   const int tiles = over_all([&](const Seq& s, int heads) { return heads * ((s.tiles >> p.tile_shift) + 1); });   // in units of 2^tile_shift, which add up in 32 bits
-  auto splits_at = [](const Seq& s, int share) { return max(1, ceil_ratio(s.tiles, share)); };
-  auto used_at = [&](int share) { return over_all([&](const Seq& s, int heads) { return heads * splits_at(s, share); }); };
+  // By floats: all that counts is that every wavefront finds the same number, and that the sum fits the grid.
+  auto splits_at = [](const Seq& s, float per_tile) { return max(1, (int)ceilf((float)s.tiles * per_tile)); };
+  auto used_at = [&](int share) {
+    const float per_tile = __builtin_amdgcn_rcpf((float)share);
+    return over_all([&](const Seq& s, int heads) { return heads * splits_at(s, per_tile); });
+  };
   // The host launches more workgroups than there can be items: this share is enough, and the least that is lies between N / W and it.
-  int share = (ceil_ratio(tiles, p.workgroups - items) << p.tile_shift) + 1;
-  int used;
-  if (share <= p.least_tiles) {
-    used = used_at(share = p.least_tiles);
-  } else {
-    int too_small = max(p.least_tiles - 1, (tiles / p.workgroups << p.tile_shift) - 1);
+  const float unit = (float)(1 << p.tile_shift), all = (float)tiles * unit;
+  int share = max(p.least_tiles, (int)(all * __builtin_amdgcn_rcpf((float)(p.workgroups - items)) * 1.0001f) + 2), used = used_at(share);
+  if (share > p.least_tiles) {
+    int too_small = max(p.least_tiles - 1, (int)(all * __builtin_amdgcn_rcpf((float)p.workgroups) * 0.9999f - unit) - 1);
     for (int i = 0; i < 5 && share - too_small > 1; ++i) {
-      const int middle = too_small + (share - too_small) / 2;
-      if (used_at(middle) <= p.workgroups) share = middle;
+      const int middle = too_small + (share - too_small) / 2, u = used_at(middle);
+      if (u <= p.workgroups) { share = middle; used = u; }
       else too_small = middle;
     }
-    used = used_at(share);
   }
+  while (used > p.workgroups) used = used_at(share += share / 8 + 1);   // not reached but by rounding
   if ((int)blockIdx.x >= used) return false;
   w.past_caches = p.max_blocks == 1 && (int64_t)tiles << p.tile_shift >= p.caches_tiles;
   const int id = chunked_id(p, blockIdx.x, used);
   int before = 0;
   for (int b0 = 0; b0 < p.batch; b0 += kWave) {
     const Seq s = sequence_at(b0);
-    const int splits = splits_at(s, share), here = p.hkv * s.blocks * splits, upto = wave_scan(here);
+    const int splits = splits_at(s, __builtin_amdgcn_rcpf((float)share)), here = p.hkv * s.blocks * splits, upto = wave_scan(here);
     const uint64_t past = __ballot(id < before + upto);
     if (past) {
       const int l = __builtin_ctzll(past);
