@@ -75,7 +75,10 @@ hipError_t launch_paged_merge(const PagedAttnParams& p, hipStream_t s) {
   const int64_t cols = (int64_t)p.cache.rows * p.group;
   const int most_cols = cols < p.block_cols ? (int)cols : p.block_cols;
   const int items = p.batch * p.hkv * p.max_blocks;
-  return p.workgroups / items >= 16 ? launch_paged_merge_by<E, HD, C, 8, 8>(p, most_cols, s) : launch_paged_merge_by<E, HD, C, 1, 8>(p, most_cols, s);
+  // Eight lanes where one would have many shares to fold one round after another (a token over one head x 30000 keys 17.6 us, with one lane 19.4; a tree of 64 rows
+  // x 8/1 heads x 30000 keys 34.8, 47.2), unless the results need the machine's lanes themselves (two trees of 64 rows x 28/4 heads x 16000 keys 64.2, 56.1).
+  return p.workgroups / items >= 16 && (int64_t)items * p.block_cols * (HD / 4) <= 2 * kNumCUs * kWave
+             ? launch_paged_merge_by<E, HD, C, 8, 8>(p, most_cols, s) : launch_paged_merge_by<E, HD, C, 1, 8>(p, most_cols, s);
 }
 
 }  // namespace sdllm

@@ -70,12 +70,21 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   else if (s.window_left >= 0 && s.window_right >= 0)
     tiles = std::min<int64_t>(tiles, ((int64_t)s.window_left + s.window_right + pl.block_cols) / kTileKeys + 2 + std::min(s.sinks, capacity) / kTileKeys);
   // With few items a workgroup has the eight wavefronts that a CU's LDS has room for, with many of them two of four wavefronts share it, one starting or
-  // merging while the other streams.
+  // merging while the other streams.  Single tokens: 64 items of 4000 keys 26.6 us with eight, 28.1 with four; 128 of 1000 to 16000 keys 96.9, 93.9; 256 of
+  // 2000 keys 49.7, 47.2.
   pl.waves = f32 ? paged_waves_f32(s.head_dim) : !pl.shared && items > 64 ? 4 : 8;
   const int64_t at_once = !f32 && pl.waves == 4 ? 2 * kNumCUs : kNumCUs;
-  pl.least_tiles = f32 ? 2 * pl.waves : pl.shared ? 8 : 6 * pl.waves;
-  // A second round of workgroups that share columns' keys costs more than uneven items do
-  pl.splits = items <= (pl.shared ? 160 : 2 * at_once) && tiles > pl.least_tiles;
+  // Shares pay for a second launch, 4 to 5 us.  Up to 32 items leave most CUs idle without them: a tile for every wavefront is enough (us by tiles of a share:
+  // 8 heads x 4096 keys, trees of 8 rows 13.3 with 8, 14.9 with 16, 18.8 with 48; 32 heads x 2000 keys, a token 12.2, 13.1, 15.5; 8 heads x 500 keys in fp32
+  // 12.3 with 4, 15.2 with 8), where uncut items have four rounds of them at least (8 heads x 600 keys, a token: 10.4 with 8, 8.4 uncut; x 1000 keys 11.0, 11.0).
+  // More items want larger ones: 64 heads x 1000 keys, a token 12.8 with 8, 11.9 with 24; 64 x 500 keys in fp32 17.8 with 4, 16.4 with 8.
+  // Shared tiles: 16 heads x 1000 keys x 224 columns 21.9 us with 4 or 8, 26.5 with 16, 31.0 with 32.
+  const bool few = !pl.shared && items <= 32;
+  pl.least_tiles = few ? pl.waves : pl.shared ? 8 : f32 ? 2 * pl.waves : 6 * pl.waves;
+  // With items for half the CUs, workgroups that share tiles are better left whole: a second round of them costs more than uneven items do (256 columns x 2000
+  // keys: 128 items 63.1 us cut, 77.7 whole; 160 items 102, 78.1).  Streaming ones fit in between (320 items of 2000 keys 63.0 cut, 59.9 whole, of 1 to 8000
+  // keys 128, 151).
+  pl.splits = items <= (pl.shared ? kNumCUs / 2 : 2 * at_once) && tiles > (few ? 4 * pl.waves - 1 : pl.least_tiles);
   pl.workgroups = pl.splits ? (int)std::max<int64_t>(at_once, 2 * items) : (int)items;
   while (tiles >> pl.tile_shift >= 1 << 20) ++pl.tile_shift;   // items <= 1024
   return SDLLM_OK;

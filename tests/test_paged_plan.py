@@ -50,13 +50,16 @@ def test_fp32_streams():
 
 
 def test_shares():
-    assert plan(1, 28, 4, 1) == (0, 16, 8, 256, 48)                    # few items: workgroups of eight
+    assert plan(1, 28, 4, 1) == (0, 16, 8, 256, 8) and plan(32, 1, 1, 1) == (0, 16, 8, 256, 8)   # few items: a tile for every wavefront is a share
+    assert plan(33, 1, 1, 1) == (0, 16, 8, 256, 48)
     assert plan(64, 1, 1, 1) == (0, 16, 8, 256, 48) and plan(65, 1, 1, 1) == (0, 16, 4, 512, 24)
     assert plan(512, 1, 1, 1) == (0, 16, 4, 1024, 24) and plan(1024, 1, 1, 1) == (0, 16, 4, 2048, 24)
     assert plan(1025, 1, 1, 1) == (0, 16, 4, 1025, 0)                  # more: nothing is cut
-    assert plan(1, 28, 4, 1, capacity=1024)[3:] == (4, 0)              # nor where no block has more tiles than a share
-    assert plan(1, 28, 4, 1, window_left=1023, sinks=4)[3:] == (4, 0) and plan(1, 28, 4, 1, window_left=4000)[3:] == (256, 48)
-    assert plan(40, 256, 4, 4) == (1, 256, 8, 320, 8) and plan(41, 256, 4, 4) == (1, 256, 8, 164, 0)
+    assert plan(1, 28, 4, 1, capacity=992)[3:] == (4, 0) and plan(1, 28, 4, 1, capacity=1024)[3:] == (256, 8)   # nor where there are few tiles
+    assert plan(33, 1, 1, 1, capacity=1536)[3:] == (33, 0) and plan(33, 1, 1, 1, capacity=1600)[3:] == (256, 48)
+    assert plan(1, 28, 4, 1, window_left=900, sinks=4)[3:] == (4, 0) and plan(1, 28, 4, 1, window_left=4000)[3:] == (256, 8)
+    assert plan(8, 4, 4, 2, dtype="f32")[3:] == (256, 4) and plan(9, 4, 4, 2, dtype="f32")[3:] == (256, 8)
+    assert plan(32, 256, 4, 4) == (1, 256, 8, 256, 8) and plan(33, 256, 4, 4) == (1, 256, 8, 132, 0)
     assert plan(8, 28, 4, 64, op=TREE) == (1, 256, 8, 256, 8)
     assert plan(4, 28, 4, 4096) == (1, 256, 8, 4 * 4 * 112, 0)
 
