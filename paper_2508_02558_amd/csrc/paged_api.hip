@@ -62,7 +62,10 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   pl.max_blocks = (int)((cols + pl.block_cols - 1) / pl.block_cols);
   if (heads > INT32_MAX) return SDLLM_ERR_UNSUPPORTED;
   const int64_t items = heads * pl.max_blocks;
-  if (items > UINT32_MAX / (kGeneralMaxWaves * kWave)) return SDLLM_ERR_UNSUPPORTED;
+  const int chunks = std::max(1, (pl.max_blocks + 3) / 4);   // neighbours that are started together: four, or nearly
+  pl.chunk = (pl.max_blocks + chunks - 1) / chunks;
+  const int64_t whole = heads * chunks * pl.chunk;   // workgroups of items that are not cut
+  if (whole > UINT32_MAX / (kGeneralMaxWaves * kWave)) return SDLLM_ERR_UNSUPPORTED;
   // tiles of an item, at most
   const int capacity = capacity_of(s);
   int64_t tiles = (capacity + kTileKeys - 1) / kTileKeys;
@@ -85,7 +88,7 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   // keys: 128 items 63.1 us cut, 77.7 whole; 160 items 102, 78.1).  Streaming ones fit in between (320 items of 2000 keys 63.0 cut, 59.9 whole, of 1 to 8000
   // keys 128, 151).
   pl.splits = items <= (pl.shared ? kNumCUs / 2 : 2 * at_once) && tiles > (few ? 4 * pl.waves - 1 : pl.least_tiles);
-  pl.workgroups = pl.splits ? (int)std::max<int64_t>(at_once, 2 * items) : (int)items;
+  pl.workgroups = pl.splits ? (int)std::max<int64_t>(at_once, 2 * items) : (int)whole;
   while (tiles >> pl.tile_shift >= 1 << 20) ++pl.tile_shift;   // items <= 1024
   return SDLLM_OK;
 }
@@ -148,8 +151,10 @@ int32_t run_paged(const sdllm_paged_shape_t* shape, bool tree, const void* q, co
     p.item_at = (int32_t*)((char*)ws + bytes.part_o + bytes.part_ml);
   }
   p.caches_tiles = (128 << 20) / (2 * kTileKeys * s.head_dim * elem_size(s.dtype));
-  p.chunk = std::min(pl.max_blocks, 4);
-  p.by_chunk = Divisor((uint32_t)p.chunk);
+  p.chunk = pl.chunk;
+  p.heads = s.batch * s.n_kv_heads;
+  p.turned = p.heads % 2 == 0 ? 5 : 0;
+  p.by_chunk = Divisor((uint32_t)p.chunk); p.by_heads = Divisor((uint32_t)p.heads);
   p.by_group = Divisor((uint32_t)p.group); p.by_blocks = Divisor((uint32_t)p.max_blocks); p.by_hkv = Divisor((uint32_t)p.hkv);
   return launch_attn_paged(p, pl, tree ? kSeeTree : kSeeWindow, s.dtype, s.head_dim, (hipStream_t)stream) == hipSuccess ? SDLLM_OK : SDLLM_ERR_HIP;
 }

@@ -26,7 +26,8 @@ struct PagedItem {
 
 // Workgroup ids are dealt round-robin over the XCDs, and by each XCD over its shader engines, without regard to how long a workgroup takes.  So is the
 // work: every XCD takes `chunk` neighbours, which read the same keys, of every 8 chunk ids, and every other turn goes backwards over XCDs and neighbours,
-// so that ids in descending order of work come out even.  (Contiguous ranges, xcd_contiguous_id, give an XCD whole sequences.)
+// so that ids in descending order of work come out even.  (Contiguous ranges, xcd_contiguous_id, give an XCD whole sequences: prompts of unlike lengths took 319
+// us instead of 237.)  chunk is 4: 2 and 8 were 4 and 6 % slower on prompts of unlike lengths.
 __device__ __forceinline__ int chunked_id(const PagedAttnParams& p, int dealt, int n) {
   const int x = dealt % kNumXCDs, s = dealt / kNumXCDs, turn = p.by_chunk.quotient(s), e = s - turn * p.chunk;
   if (dealt >= p.by_chunk.quotient(n / kNumXCDs) * p.chunk * kNumXCDs) return dealt;
@@ -97,16 +98,20 @@ __device__ __forceinline__ void locate_item(const PagedAttnParams& p, PagedItem&
 template <int SEES>
 __device__ __forceinline__ bool find_item(const PagedAttnParams& p, int lane, PagedItem& w) {
   if (!p.part_o) {
-    // Items as workgroups, the last block of a head first: with all past keys to see it has the most tiles
+    // Items as workgroups: `chunk` neighbouring blocks of a head, then those of the other heads, from the last blocks to the first: with all past keys to see the
+    // last have the most tiles, and those that are not there come at the end.  (One head after another: causal, 32 heads x 4096 rows 257 us instead of 180, two
+    // sequences of 2048 rows x 28/4 heads 114 instead of 78.)  The heads' order turns from chunk to chunk, or the ones whose sequences are long would stay
+    // on a few XCDs (four sequences of 1024 to 4096 rows x 28/4 heads, a window of 1024 keys: 215 us, unturned 250).
     const int id = chunked_id(p, blockIdx.x, gridDim.x);
-    const int head = p.by_blocks.quotient(id), rank = id - head * p.max_blocks;
+    const int unit = p.by_chunk.quotient(id), turn = p.by_heads.quotient(unit), place = unit + turn * p.turned;
+    const int head = place - p.by_heads.quotient(place) * p.heads, rank = id + (turn - unit) * p.chunk;
     w.b = p.by_hkv.quotient(head);
     w.g = head - w.b * p.hkv;
     w.count = __builtin_amdgcn_readfirstlane(p.cache.count(w.b));
+    w.length = __builtin_amdgcn_readfirstlane(p.cache.length(w.b));
     const int blocks = blocks_of(p, w.count);
     if (rank >= blocks) return false;
     w.blk = blocks - 1 - rank;
-    w.length = __builtin_amdgcn_readfirstlane(p.cache.length(w.b));
     w.split = 0;
     w.n_split = 1;
     w.slot = 0;

@@ -343,7 +343,8 @@ struct PagedAttnParams {
   int32_t tile_shift;                 // in units of 2^tile_shift the tiles of all items add up in 32 bits
   int32_t caches_tiles;               // tiles from which on they are read past the caches
   int32_t chunk;                      // neighbours among the workgroups that go to one XCD
-  Divisor by_group, by_blocks, by_hkv, by_chunk;
+  int32_t heads, turned;              // batch x hkv; places that their order turns by from one chunk of blocks to the next
+  Divisor by_group, by_blocks, by_hkv, by_chunk, by_heads;
 };
 
 // Most wavefronts of a workgroup: with fp32 tensors the three parts of the queries take the registers of two
@@ -354,7 +355,7 @@ hipError_t launch_attn_packed(const PackedAttnParams& p, int dtype, int d, hipSt
 hipError_t launch_qk_norm_rope(const QkParams& p, int dtype, int d, hipStream_t s);
 hipError_t launch_append_paged(const AppendParams& p, int dtype, int d, hipStream_t s);
 // how a call is cut up
-struct PagedPlan { bool shared; int block_cols, waves, max_blocks, workgroups, least_tiles, tile_shift; bool splits; };
+struct PagedPlan { bool shared; int block_cols, waves, max_blocks, chunk, workgroups, least_tiles, tile_shift; bool splits; };
 constexpr int paged_waves_f32(int d) { return d == 128 ? 4 : 8; }   // that a CU's LDS has room for
 hipError_t launch_attn_paged(const PagedAttnParams& p, const PagedPlan& pl, int sees, int dtype, int d, hipStream_t s);
 hipError_t launch_attn_paged_shared(const PagedAttnParams& p, const PagedPlan& pl, int sees, int d, hipStream_t s);
