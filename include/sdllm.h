@@ -339,7 +339,8 @@ int32_t sdllm_qk_norm_rope(const sdllm_qk_shape_t* shape, const void* q_in, cons
  * Integers are device memory, so that a captured graph takes those of its replay.  Pages are never allocated, moved or cleared.
  *
  * Both attentions run with fp32 sums; with bf16 tensors the softmax numerators are rounded to bf16 for the product with the values.  A row that sees no
- * key is zero.  What a row does not see takes no part in its result, whatever it holds (infinities and NaN included).
+ * key is zero.  What a row does not see takes no part in its result, whatever it holds (infinities and NaN included).  Outputs and workspace may overlap
+ * nothing else; calls that may run at the same time, on two streams or in two graphs, need a workspace each.
  */
 typedef struct sdllm_paged_shape {
   int32_t batch;        /* B >= 1 sequences */

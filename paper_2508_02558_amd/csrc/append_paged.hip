@@ -1,6 +1,7 @@
 // Appending to the paged cache: norm and rotation of the new queries and keys as in qk_norm_rope.hip, the keys, and the values as they
 // are, stored in the rows that the page table names.  Bound by memory: everything is read and written once.  A wavefront takes heads of one new row; a
-// row's place is found once per wavefront, while its heads are on their way.
+// row's place is found once per wavefront, while its heads are on their way.  8 sequences of 1024 to 4096 rows x 32/8 heads of 128: 503 MB in 95 us, 5.3 TB/s (a
+// copy: 5.1); one token of 28/4 heads 3.3 us, two round trips to memory and the launch.
 #include "qk_rope_math.h"
 
 namespace sdllm {
@@ -90,6 +91,7 @@ hipError_t launch_as(const AppendParams& a, hipStream_t s) {
   constexpr int kHeads = kWave * 2 * Piece<T>::N / HD;
   const int passes = (q.hq + q.hkv + kHeads - 1) / kHeads + (q.hkv + kHeads - 1) / kHeads;
   // as in qk_norm_rope.hip: wavefronts per row until there are four for every SIMD, few of them spread over all CUs, much data past the caches
+  // (bf16, 32/8 heads, MB read and written: 384 77 us, through the caches 84; 768 148, 158; 192 43, 48, but that much the next call finds in the memory-side cache)
   q.parts = 1;
   while (q.parts < passes && (int64_t)q.tokens * q.parts < 16 * kNumCUs) q.parts *= 2;
   if (q.parts > passes) q.parts = passes;

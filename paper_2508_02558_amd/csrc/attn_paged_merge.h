@@ -1,6 +1,7 @@
 // Merge of the shares of the paged cache's attention: what the workgroups of an item left, folded with the usual rescaling, as a launch of its own.
 // An item's first workgroup says where its partials are and how many (item_at).  Bound by round trips: the item's place, then everything else
-// of several shares at once, with many shares by eight lanes that take every eighth each.
+// of several shares at once, with many shares by eight lanes that take every eighth each.  64 blocks of 256 columns x 128 in four shares (33 MB) 8.6 us, 128 of
+// 16 columns 4.9.
 #pragma once
 
 #include "attn_merge.h"

@@ -200,6 +200,15 @@ def test_pages_beyond_32_bit_offsets():
             assert torch.equal(k[page_at, 0, (length + i) % page], rows[b, 0, i]) and torch.equal(v[page_at, 0, (length + i) % page], rows[b, 0, i])
 
 
+@pytest.mark.parametrize("kind,Hq,Hkv,n,lengths", [("window", 8, 2, 1, (5000, 900, 33)), ("tree", 28, 4, 40, (700, 2000, 0)), ("window", 16, 1, 64, (1500, 300, 7))])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pages_named_more_than_once(kind, Hq, Hkv, n, lengths, dtype):
+    c = Paged(kind, Hq, Hkv, 64, n, lengths, dtype, page_rows=32, mask=tree_masks(3, n, 1) if kind == "tree" else None)
+    c.table[:] = c.table[0, :3].repeat(c.table.shape[1])[:c.table.shape[1]]   # all sequences share three pages, again and again
+    c.run()
+    c.check()
+
+
 # the forms of the attentions: streaming or shared tiles, columns, wavefronts, cut or not
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("kind,Hq,Hkv,n,lengths,form", [
