@@ -872,7 +872,7 @@ const char* sdllm_error_string(int32_t status) {
   }
 }
 
-int32_t sdllm_version(void) { return 200; }
+int32_t sdllm_version(void) { return 300; }
 
 int32_t sdllm_retained_count(const sdllm_shape_t* shape, int32_t* k_total, int32_t* k_pre, int32_t* k_suf) {
   const int32_t st = check_shape(shape);
