@@ -60,12 +60,12 @@ struct Step {
   static __device__ __forceinline__ int v_col(int i) { return i % NE; }
 };
 
-// Numerators r and r + 1 of 16 keys (eight in this lane), keys 16 part .. of the step
-template <int KT>
-__device__ __forceinline__ void numerator_pair(const f32x16 (&s)[KT], int part, int r, float scale_log2, float m_ref, float& l, bf16x8 (&pb)[2 * KT]) {
+// Numerators r and r + 1 of 16 keys (eight in this lane), keys 16 part .. of the step, of exponents `at`
+template <int KT, class At>
+__device__ __forceinline__ void numerator_pair(const At& at, int part, int r, float& l, bf16x8 (&pb)[2 * KT]) {
 #pragma unroll
   for (int i = r; i < r + 2; ++i) {
-    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[part >> 1][8 * (part & 1) + i], scale_log2, -m_ref));
+    const float x = __builtin_amdgcn_exp2f(at(part, i));
     l += x;
     pb[part][i] = (__bf16)x;
   }
@@ -87,8 +87,9 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
 
   PagedItem w;
   if (!find_item<SEES>(p, lane, w)) return;
-  const int per_split = ceil_div(w.tiles, w.n_split);
-  const int t0 = min(w.tiles, w.split * per_split), n_tiles = min(w.tiles - t0, per_split);
+  // the same for all lanes, and known to be: the loop's branches are scalar
+  const int per_split = __builtin_amdgcn_readfirstlane(ceil_div(w.tiles, w.n_split));
+  const int t0 = __builtin_amdgcn_readfirstlane(min(w.tiles, w.split * per_split)), n_tiles = __builtin_amdgcn_readfirstlane(min(w.tiles - t0, per_split));
   const int nsteps = ceil_div(n_tiles, KS * KT);   // step j, group k: tiles t0 + (j KS + k) KT ..
 
   // columns past the last compute on a copy of it and are not written back
@@ -183,6 +184,7 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
     bf16x8 a[8], pb[2 * KT];
     i16x8 f[8];
     f32x16 sn[KT];
+    float late_at[KT][8];   // exponents of the second half, so that the logits' registers are free for the next step's from its first product on
 
     bool full;
     auto mask = [&](int step) __attribute__((always_inline)) {
@@ -196,6 +198,8 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
         mask_logits(sn[q], n0 + q >= n_tiles ? 0u : seen_bits<SEES>(p, x, sight), half);
       }
     };
+    auto exponent = [&](int part, int i) __attribute__((always_inline)) { return __builtin_fmaf(sn[part >> 1][8 * (part & 1) + i], p.scale_log2, -m_run); };
+    auto late_exponent = [&](int part, int i) __attribute__((always_inline)) { return late_at[part - KT][i]; };
     // Vector phase of a step: masks, row maxima, the reference, first half of the numerators
     auto vector_phase = [&](int step) __attribute__((always_inline)) {
       mask(step);
@@ -209,21 +213,22 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
 #pragma unroll
       for (int part = 0; part < KT; ++part)
 #pragma unroll
-        for (int r = 0; r < 8; r += 2) numerator_pair<KT>(sn, part, r, p.scale_log2, m_run, l, pb);
+        for (int r = 0; r < 8; r += 2) numerator_pair<KT>(exponent, part, r, l, pb);
       l_run += l;
+#pragma unroll
+      for (int part = 0; part < KT; ++part)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) late_at[part][r] = exponent(KT + part, r);
       if (!full) specials |= take_specials(f);
     };
     // Matrix phase: logits of the next step, second product of the current one, each operand register set reloaded for the next phase once it has been
     // used; the other half of the current step's numerators between the first instructions.
     auto matrix_phase = [&](int k_slot, int v_slot) __attribute__((always_inline)) {
-      f32x16 s[KT];
       float l = 0.f;
 #pragma unroll
-      for (int q = 0; q < KT; ++q) {
-        s[q] = sn[q];
+      for (int q = 0; q < KT; ++q)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sn[q][i] = 0.f;
-      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         sn[S::k_tile(i)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], qf[S::k_part(i)], sn[S::k_tile(i)], 0, 0, 0);
@@ -234,7 +239,7 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
 #pragma unroll
           for (int j = 0; j < KT; ++j) {
             const int n = i * KT + j;   // pair: keys of the second half in order
-            numerator_pair<KT>(s, KT + n / 4, n % 4 * 2, p.scale_log2, m_run, l, pb);
+            numerator_pair<KT>(late_exponent, KT + n / 4, n % 4 * 2, l, pb);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -315,7 +320,7 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
 #pragma unroll
     for (int part = KT; part < 2 * KT; ++part)
 #pragma unroll
-      for (int r = 0; r < 8; r += 2) numerator_pair<KT>(sn, part, r, p.scale_log2, m_run, l, pb);
+      for (int r = 0; r < 8; r += 2) numerator_pair<KT>(late_exponent, part, r, l, pb);
     l_run += l;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
