@@ -139,39 +139,46 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
     const int my_row = S::fetch_row(wave, lane);
     const uint32_t off_k = (uint32_t)(my_row & (kTileKeys - 1)) * item.stride + S::fetch_k_piece(lane);
     const uint32_t off_v = (uint32_t)(my_row & (kTileKeys - 1)) * item.stride + S::fetch_v_piece(lane);
-    auto fetch = [&](bool is_v, int step, int slot) __attribute__((always_inline)) {
+    struct From { const char* group[KS]; };
+    auto from = [&](bool is_v, int step) __attribute__((always_inline)) {
       const char *pages = is_v ? item.v : item.k, *own = is_v ? item.v_own : item.k_own;
       const uint32_t off = is_v ? off_v : off_k;
+      From r;
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
-        const uint32_t to = lds0 + (uint32_t)(slot + (is_v ? kV0 + i * kRingV + wave * kVGroup : i * kRingK + wave * kKGroup));
         const int n = (step * KS + i) * KT, n0 = min(n, n_tiles - 1) & 63, n1 = min(n + KT - 1, n_tiles - 1) & 63;
         const uint32_t bits0 = (uint32_t)__builtin_amdgcn_readlane((int)places.bits, n0), bits1 = (uint32_t)__builtin_amdgcn_readlane((int)places.bits, n1);
         if (bits0 & bits1 & kWhole) {
           const int64_t a = readlane64(places.at0, n0);
           if constexpr (KT == 1) {
-            fetch_to_lds(to, pages + a, off);
+            r.group[i] = pages + a + off;
           } else {
             const int64_t b = readlane64(places.at0, n1);
-            fetch_to_lds(to, pages + (my_row >= kTileKeys ? b : a) + off);
+            r.group[i] = pages + (my_row >= kTileKeys ? b : a) + off;
           }
         } else {
           int l = lane;
           asm volatile("" : "+v"(l));   // worked out here, not kept
           const int row = S::fetch_row(wave, l);
           const TilePlace a = place_from(places, n0);
-          const char* from = (a.bits & kOwn ? own : pages) + row_at(a, item, row & (kTileKeys - 1));
+          const char* at = (a.bits & kOwn ? own : pages) + row_at(a, item, row & (kTileKeys - 1));
           if constexpr (KT > 1) {
             const TilePlace b = place_from(places, n1);
             const char* other = (b.bits & kOwn ? own : pages) + row_at(b, item, row & (kTileKeys - 1));
-            from = row >= kTileKeys ? other : from;
+            at = row >= kTileKeys ? other : at;
           }
-          fetch_to_lds(to, from + (is_v ? S::fetch_v_piece(l) : S::fetch_k_piece(l)));
+          r.group[i] = at + (is_v ? S::fetch_v_piece(l) : S::fetch_k_piece(l));
         }
       }
+      return r;
     };
-    auto fetch_k = [&](int step, int slot) __attribute__((always_inline)) { fetch(false, step, slot); };
-    auto fetch_v = [&](int step, int slot) __attribute__((always_inline)) { fetch(true, step, slot); };
+    auto fetch = [&](bool is_v, const From& x, int slot) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+        fetch_to_lds(lds0 + (uint32_t)(slot + (is_v ? kV0 + i * kRingV + wave * kVGroup : i * kRingK + wave * kKGroup)), x.group[i]);
+    };
+    auto fetch_k = [&](int step, int slot) __attribute__((always_inline)) { fetch(false, from(false, step), slot); };
+    auto fetch_v = [&](int step, int slot) __attribute__((always_inline)) { fetch(true, from(true, step), slot); };
     // The 64 tiles at hand change before the K of a step that begins with the next; V of the step before has been asked for by then.
     auto turn_page = [&](int step) __attribute__((always_inline)) {
       const int n = step * KS * KT;
@@ -187,11 +194,14 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
     float late_at[KT][8];   // exponents of the second half, so that the logits' registers are free for the next step's from its first product on
 
     bool full;
-    auto mask = [&](int step) __attribute__((always_inline)) {
+    auto look_ahead = [&](int step) __attribute__((always_inline)) {   // full: every row of this wave sees all of the step's tiles
       const int n0 = (step * KS + kg) * KT;
       const uint64_t whole = (n0 >> 6 == at_hand ? whole_now : whole_before) >> (n0 & 63);
       full = (~whole & ((1u << KT) - 1)) == 0;
+    };
+    auto mask = [&](int step) __attribute__((always_inline)) {
       if (full) return;
+      const int n0 = (step * KS + kg) * KT;
 #pragma unroll
       for (int q = 0; q < KT; ++q) {
         const PagedTile x = tile_of<SEES>(p, w, t0 + min(n0 + q, n_tiles - 1));
@@ -222,8 +232,9 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
       if (!full) specials |= take_specials(f);
     };
     // Matrix phase: logits of the next step, second product of the current one, each operand register set reloaded for the next phase once it has been
-    // used; the other half of the current step's numerators between the first instructions.
-    auto matrix_phase = [&](int k_slot, int v_slot) __attribute__((always_inline)) {
+    // used; the other half of the current step's numerators between the first instructions, `between(i)` (scalar work that the vector phase would wait for)
+    // between the others.
+    auto matrix_phase = [&](int k_slot, int v_slot, const auto& between) __attribute__((always_inline)) {
       float l = 0.f;
 #pragma unroll
       for (int q = 0; q < KT; ++q)
@@ -242,6 +253,7 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
             numerator_pair<KT>(late_exponent, KT + n / 4, n % 4 * 2, l, pb);
           }
         }
+        between(i);
         __builtin_amdgcn_sched_barrier(0);
       }
       l_run += l;
@@ -276,6 +288,7 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
     for (int i = 0; i < 8; ++i) f[i] = S::v_frag(v_at, i);
 #pragma unroll
     for (int i = 0; i < 8; ++i) a[i] = S::k_frag(k_at + kStepK, i);
+    look_ahead(0);
     vector_phase(0);
     // What the early waves read before a wait of the late ones stands between has landed: K(2), K(3), V(1), V(2).
     if (KS == 1) asm volatile("s_waitcnt lgkmcnt(0) vmcnt(3)" ::: "memory");   // V(3), K(4), V(4)
@@ -296,14 +309,21 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
     int t = 0, v_slot = kStepV, k_slot = 2 * kStepK, v_next = 0, k_next = kStepK;   // places of V(t+1), K(t+2), V(t+N), K(t+N+1)
     auto advance = [&](int& slot, int by) __attribute__((always_inline)) { slot = slot + by == N * by ? 0 : slot + by; };
     auto iteration = [&](auto fetches) __attribute__((always_inline)) {
+      From v_from, k_from;
       __builtin_amdgcn_s_setprio(1);
-      matrix_phase(k_slot, v_slot);
+      matrix_phase(k_slot, v_slot, [&](int i) __attribute__((always_inline)) {
+        if (fetches && i == 4) v_from = from(true, t + N);
+        if (fetches && i == 5) {
+          turn_page(t + N + 1);
+          k_from = from(false, t + N + 1);
+        }
+        if (i == 6) look_ahead(t + 1);
+      });
       __builtin_amdgcn_s_setprio(0);
       bare_barrier();
       if (fetches) {
-        fetch_v(t + N, v_next);
-        turn_page(t + N + 1);
-        fetch_k(t + N + 1, k_next);
+        fetch(true, v_from, v_next);
+        fetch(false, k_from, k_next);
       }
       in_issue_order();
       vector_phase(t + 1);
