@@ -29,8 +29,10 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
 
   PagedItem w;
   if (!find_item<SEES>(p, lane, w)) return;
-  const int per_split = ceil_div(w.tiles, w.n_split);
-  const int t_begin = min(w.tiles, w.split * per_split) + wave, t_end = min(w.tiles, (w.split + 1) * per_split);
+  // the same for all lanes, and known to be: the loop's branches are scalar
+  const int per_split = __builtin_amdgcn_readfirstlane(ceil_div(w.tiles, w.n_split));
+  const int t_begin = __builtin_amdgcn_readfirstlane(min(w.tiles, w.split * per_split)) + wave;
+  const int t_end = __builtin_amdgcn_readfirstlane(min(w.tiles, (w.split + 1) * per_split));
   const int n_mine = max(0, (t_end - t_begin + NW - 1) / NW);   // tiles t_begin, t_begin + NW, ...
 
   const int column = w.blk * C + col, in = min(column, w.cols - 1);
