@@ -4,12 +4,13 @@
 // on block w % (8 / KS) of 32 columns and, of KS key groups, on group w / (8 / KS).  A step of a group is 8 KB of K and of V, one tile of head_dim 128 or two of
 // head_dim 64, so that both have sixteen matrix instructions a step.  The two waves of a SIMD are locked in opposite phases, with a barrier at each change, as in
 // dense_full_mfma.hip, which says why: while one issues its matrix instructions (logits of step t+1 between the second product of
-// step t), the other finds row maxima and does the first half of its exponentials.
+// step t), the other finds row maxima and does the first half of its exponentials.  The vector phase would be the longer one, so where the next tiles are, and which
+// of them are masked, is worked out in the matrix phase: causal with head_dim 64 240 us became 200.
 // Tiles that some row of a wave does not see all of are masked by 32 bits per row (seen_bits); whole tiles pay one scalar test.  Pages of the next 64 tiles are
 // looked up by one load, a tile per lane.
-// Rates, of 1245 TFLOP/s that a large product reaches: 4 x 4096 rows x 28/4 heads of 128, all keys seen, 930 to 1000 (without pages 1100), causal 905; four
-// prompts of 1024 to 4096 rows with a window of 1024 keys 660 (216 us; of a workgroup's 50 us 7 pass until its first logits, and the fifth round of workgroups is a
-// third full); head_dim 64, 8192 rows x 16/2 heads, causal, 700 (247 us, twice the exponentials per product).
+// Rates, of 1245 TFLOP/s that a large product reaches: 4 x 4096 rows x 28/4 heads of 128, all keys seen, 1016 (without pages 1100), causal 970 to 990; four
+// prompts of 1024 to 4096 rows with a window of 1024 keys 720 (198 us; 7 of a workgroup's 45 us pass until its first logits, and the fifth round of workgroups is a
+// third full); head_dim 64, 8192 rows x 16/2 heads, causal, 855 (200 us, twice the exponentials per product).
 #include <type_traits>
 
 #include "attn_paged_merge.h"

@@ -55,7 +55,7 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   const int64_t heads = (int64_t)s.batch * s.n_kv_heads;
   // 16 columns are enough for a token's heads and take less than 32 with half of them empty (a token of 4 sequences of 1000 keys x 28/4 heads 10.9 us, 11.8).
   // Up to 64 columns two blocks that read the same tiles, one of them from L2, are ahead of waves that share them (8 trees of 16 rows x 32/8 heads x 4096 rows
-  // 33.7 us, shared 42.5), up to 128 where there are few heads (one tree of 32 rows x 32/8 heads x 8192 rows 21.5, shared 27.2; 8 trees 46.0, 44.7).
+  // 33.2 us, shared 38.8), up to 128 where there are few heads (one tree of 32 rows x 32/8 heads x 8192 rows 21.5, shared 26.0; 8 trees 44.4, 40.0).
   pl.shared = !f32 && cols > (heads <= 16 ? 128 : 64);
   pl.block_cols = f32 || cols <= 16 ? 16 : !pl.shared ? 32 : cols <= 128 ? 128 : 256;
   // columns, blocks and threads of a launch (the merge's too) are counted in 32 bits
@@ -82,11 +82,11 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   // 8 heads x 4096 keys, trees of 8 rows 13.3 with 8, 14.9 with 16, 18.8 with 48; 32 heads x 2000 keys, a token 12.2, 13.1, 15.5; 8 heads x 500 keys in fp32
   // 12.3 with 4, 15.2 with 8), where uncut items have four rounds of them at least (8 heads x 600 keys, a token: 10.4 with 8, 8.4 uncut; x 1000 keys 11.0, 11.0).
   // More items want larger ones: 64 heads x 1000 keys, a token 12.8 with 8, 11.9 with 24; 64 x 500 keys in fp32 17.8 with 4, 16.4 with 8.
-  // Shared tiles: 16 heads x 1000 keys x 224 columns 21.9 us with 4 or 8, 26.5 with 16, 31.0 with 32.
+  // Shared tiles: 8 heads x 1000 keys x 224 columns 18.8 us with 4, 18.4 with 8, 22.2 with 16, 25.7 with 32.
   const bool few = !pl.shared && items <= 32;
   pl.least_tiles = few ? pl.waves : pl.shared ? 8 : f32 ? 2 * pl.waves : 6 * pl.waves;
   // With items for half the CUs, workgroups that share tiles are better left whole: a second round of them costs more than uneven items do (256 columns x 2000
-  // keys: 128 items 63.1 us cut, 77.7 whole; 160 items 102, 78.1).  Streaming ones fit in between (320 items of 2000 keys 63.0 cut, 59.9 whole, of 1 to 8000
+  // keys: 128 items 57.5 us cut, 66.3 whole; 144 items 91.4, 67.0).  Streaming ones fit in between (320 items of 2000 keys 63.0 cut, 59.9 whole, of 1 to 8000
   // keys 128, 151).
   pl.splits = items <= (pl.shared ? kNumCUs / 2 : 2 * at_once) && tiles > (few ? 4 * pl.waves - 1 : pl.least_tiles);
   pl.workgroups = pl.splits ? (int)std::max<int64_t>(at_once, 2 * items) : (int)whole;
