@@ -350,9 +350,15 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
   }
 
   if (specials) {
-    const int per_step = KS * KT;   // tiles of this group: KT of every step
-    add_specials<SEES>(p, w, sight, 2, 0, nsteps * KT,
-                       [&](int n) __attribute__((always_inline)) { return t0 + min(n / KT * per_step + kg * KT + n % KT, n_tiles - 1); },
+    // KT tiles of every step are this group's, and are looked at together: a whole one as well if the other is masked, or past the last
+    add_specials<SEES>(p, w, sight, 2, nsteps * KT,
+                       [&](int n) __attribute__((always_inline)) {
+                         const int n0 = (n / KT * KS + kg) * KT;
+                         bool whole = n0 + KT <= n_tiles;
+#pragma unroll
+                         for (int q = 0; q < KT; ++q) whole = whole && tile_of<SEES>(p, w, t0 + min(n0 + q, n_tiles - 1)).full;
+                         return whole ? -1 : t0 + min(n0 + n % KT, n_tiles - 1);
+                       },
                        [&](const char* v, bool sees) __attribute__((always_inline)) {
 #pragma unroll
                          for (int i = 0; i < NE * 4; ++i) {

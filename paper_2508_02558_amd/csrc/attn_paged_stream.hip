@@ -180,10 +180,15 @@ void attn_paged_stream_kernel(const PagedAttnParams p) {
   }
 
   if (specials)
-    add_specials<SEES>(p, w, sight, ES, 0, n_mine, [&](int j) { return t_begin + j * NW; }, [&](const char* v, bool sees) __attribute__((always_inline)) {
+    add_specials<SEES>(p, w, sight, ES, n_mine,
+                       [&](int j) __attribute__((always_inline)) {
+                         const int t = t_begin + j * NW;
+                         return tile_of<SEES>(p, w, t).full ? -1 : t;
+                       },
+                       [&](const char* v, bool sees) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < kSlots; ++i) T::add(acc, i, special_values<E>(v, T::channel(i, lane), sees));
-    });
+                         for (int i = 0; i < kSlots; ++i) T::add(acc, i, special_values<E>(v, T::channel(i, lane), sees));
+                       });
   const float l_tot = T::over_row(l_run, true);
   // Merge: every wavefront parks its results (slot i of a lane in place i ^ its turn) and its columns' statistics; they then share out the slots, with
   // everything that a slot needs requested at once.

@@ -264,16 +264,16 @@ __device__ __forceinline__ float or_minus_infinity(float s, uint32_t m) {
 }
 
 // Values of a masked tile that are no numbers take no part in rows that do not see them, where zero times them would be NaN.  They are taken out of the
-// operands, and a wavefront that met any goes over its masked tiles once more at the end, key by key, and adds them to the results of the rows that see
-// them: to find out costs masked tiles three instructions a pair of values, the rest nothing but where it happens.
-// `where(t)` is tile t of this wavefront's, `add(v_row, sees)` adds the infinities and NaN of one row of V.
+// operands, and a wavefront that met any goes over the tiles it looked at once more at the end, key by key, and adds them to the results of the rows that
+// see them: to find out costs masked tiles three instructions a pair of values, the rest nothing but where it happens.
+// `where(n)` is tile n of this wavefront's if its operands were looked at, or negative; `add(v_row, sees)` adds the infinities and NaN of one row of V.
 template <int SEES, class Where, class Add>
-__device__ __forceinline__ void add_specials(const PagedAttnParams& p, const PagedItem& w, const RowSight& sight, int esize, int first, int end, const Where& where,
-                                             const Add& add) {
+__device__ __forceinline__ void add_specials(const PagedAttnParams& p, const PagedItem& w, const RowSight& sight, int esize, int tiles, const Where& where, const Add& add) {
   const PagedCache& c = p.cache;
-  for (int n = first; n < end; ++n) {
-    const PagedTile x = tile_of<SEES>(p, w, where(n));
-    if (x.full) continue;
+  for (int n = 0; n < tiles; ++n) {
+    const int t = where(n);
+    if (t < 0) continue;
+    const PagedTile x = tile_of<SEES>(p, w, t);
     const uint32_t seen = seen_bits<SEES>(p, x, sight);
     for (int r = x.lo; r < x.hi; ++r) {
       const int row = x.at + r;
