@@ -350,14 +350,16 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
   }
 
   if (specials) {
-    // KT tiles of every step are this group's, and are looked at together: a whole one as well if the other is masked, or past the last
+    // KT tiles of every step are this group's, and are looked at together: a whole one as well if the other is masked, or past the last.  One past the last is
+    // a copy that counts for nothing: it may be another group's, whose rows this one has seen no key of, and zero times an infinity is NaN in the merge.
     add_specials<SEES>(p, w, sight, 2, nsteps * KT,
                        [&](int n) __attribute__((always_inline)) {
-                         const int n0 = (n / KT * KS + kg) * KT;
+                         const int n0 = (n / KT * KS + kg) * KT, t = n0 + n % KT;
+                         if (t >= n_tiles) return -1;
                          bool whole = n0 + KT <= n_tiles;
 #pragma unroll
                          for (int q = 0; q < KT; ++q) whole = whole && tile_of<SEES>(p, w, t0 + min(n0 + q, n_tiles - 1)).full;
-                         return whole ? -1 : t0 + min(n0 + n % KT, n_tiles - 1);
+                         return whole ? -1 : t0 + t;
                        },
                        [&](const char* v, bool sees) __attribute__((always_inline)) {
 #pragma unroll

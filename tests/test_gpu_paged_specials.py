@@ -39,3 +39,16 @@ def test_whole_tiles_beside_masked_ones(d, kinds, kind, Hq, n, lengths, window, 
     ("window", 40, (1000,) * 17, CAUSAL, (1, 128, 8, True)), ("tree", 40, tuple(range(60, 77)), None, (1, 128, 8, False)), ("tree", 40, (1000,) * 17, None, (1, 128, 8, True))])
 def test_whole_tiles_beside_masked_ones_with_two_key_groups(d, kind, n, lengths, window, form):
     call(kind, 2, 1, d, n, lengths, window, form=form)
+
+
+# Two key groups of a workgroup: where the tiles do not come out even, one group's tiles past the last are copies that count for nothing, whatever it has seen itself
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kinds", ["nan", "inf"])
+@pytest.mark.parametrize("kind,Hq,n,lengths,window,form", [
+    ("tree", 2, 40, tuple(range(1, 18)), None, (1, 128, 8, False)), ("tree", 4, 20, tuple(range(1, 18)), None, (1, 128, 8, False)),
+    ("tree", 2, 40, (0,) * 17, None, (1, 128, 8, False)), ("window", 2, 40, (60,) * 17, (0, 0, 0), (1, 128, 8, False)),
+    ("window", 4, 20, (20,) * 17, (0, 0, 0), (1, 128, 8, False)), ("window", 2, 40, tuple(range(100, 117)), ALL, (1, 128, 8, False)),
+    ("window", 2, 40, (88,) * 17, CAUSAL, (1, 128, 8, False)), ("tree", 2, 40, tuple(range(900, 1002, 6)), None, (1, 128, 8, True)),
+    ("window", 2, 40, tuple(range(900, 1002, 6)), CAUSAL, (1, 128, 8, True)), ("window", 2, 40, tuple(range(900, 1002, 6)), (300, 0, 7), (1, 128, 8, True))])
+def test_copies_of_the_last_tile_count_for_nothing(d, kinds, kind, Hq, n, lengths, window, form):
+    call(kind, Hq, 1, d, n, lengths, window, form=form, kinds=kinds)
