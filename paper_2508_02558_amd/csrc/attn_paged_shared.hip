@@ -104,7 +104,7 @@ void attn_paged_shared_kernel(const PagedAttnParams p) {
   // keys [most_first, least_last] are in the window of all rows of this wave
   if (SEES == kSeeWindow) {
     const int c0 = min(w.blk * kCols + rb * 32, w.cols - 1), c1 = min(w.blk * kCols + rb * 32 + 31, w.cols - 1);
-    w.least_last = last_seen<SEES>(p, w.end, w.length + p.by_group.quotient(c0));
+    w.least_last = last_seen(p, w.end, w.length + p.by_group.quotient(c0));
     w.most_first = first_seen(p, w.length + p.by_group.quotient(c1));
   }
 

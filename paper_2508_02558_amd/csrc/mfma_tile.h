@@ -92,12 +92,9 @@ __device__ __forceinline__ void fetch_to_lds(uint32_t at, const char* base, uint
 __device__ __forceinline__ void fetch_to_lds(uint32_t at, const char* lane_src) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(at), "v"(lane_src) : "memory", "m0");
 }
-// The same two past the caches, for what is read once.
+// From a base and an offset, past the caches, for what is read once.
 __device__ __forceinline__ void fetch_to_lds_once(uint32_t at, const char* base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(at), "v"(off), "s"(base) : "memory", "m0");
-}
-__device__ __forceinline__ void fetch_to_lds_once(uint32_t at, const char* lane_src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" :: "s"(at), "v"(lane_src) : "memory", "m0");
 }
 #pragma clang diagnostic pop
 // A wave-uniform address in scalar registers, where the compiler would keep it in vector registers.

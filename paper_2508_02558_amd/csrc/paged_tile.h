@@ -19,7 +19,7 @@ struct PagedItem {
   int sink_end;             // first keys that any row of the block sees as such: [0, sink_end)
   int first, last;          // keys of the window of any row: [first, last]
   int least_last, most_first;   // keys [most_first, least_last] are in the window of every row
-  bool past_caches;         // so many tiles are read in all that what is read does not stay in the caches anyway
+  bool past_caches;         // so many tiles are read in all that what is read does not stay in the caches anyway: tiles of 32 rows one stride apart are read past them
   int lead_tiles;           // tiles before the window's: of first keys, or (kSeeTree) of the cache
   int first_tile, tiles;    // first tile of the window; tiles in all
 };
@@ -48,7 +48,6 @@ __device__ __forceinline__ int wave_scan(int x) {
 }
 __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), kWave - 1); }
 
-template <int SEES>
 __device__ __forceinline__ int last_seen(const PagedAttnParams& p, int end, int place) {
   return p.right < 0 ? end - 1 : min(end - 1, place + p.right);
 }
@@ -81,8 +80,8 @@ __device__ __forceinline__ void locate_item(const PagedAttnParams& p, PagedItem&
   const int p0 = w.length + p.by_group.quotient(c0), p1 = w.length + p.by_group.quotient(c1);
   w.first = first_seen(p, p0);
   w.most_first = first_seen(p, p1);
-  w.least_last = last_seen<SEES>(p, w.end, p0);
-  w.last = last_seen<SEES>(p, w.end, p1);
+  w.least_last = last_seen(p, w.end, p0);
+  w.last = last_seen(p, w.end, p1);
   w.sink_end = min(p.sinks, w.last + 1);
   w.first_tile = w.first / kTileKeys;
   w.lead_tiles = ceil_div(w.sink_end, kTileKeys);
@@ -236,7 +235,7 @@ __device__ __forceinline__ RowSight sight_of(const PagedAttnParams& p, const Pag
     r.none = w.length == 0 && r.bits == 0;
   } else {
     r.first = first_seen(p, w.length + row);
-    r.last = last_seen<SEES>(p, w.end, w.length + row);
+    r.last = last_seen(p, w.end, w.length + row);
     r.none = r.last < 0 || (r.first > r.last && p.sinks == 0);
   }
   return r;
