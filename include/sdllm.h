@@ -339,8 +339,13 @@ int32_t sdllm_qk_norm_rope(const sdllm_qk_shape_t* shape, const void* q_in, cons
  * Integers are device memory, so that a captured graph takes those of its replay.  Pages are never allocated, moved or cleared.
  *
  * Both attentions run with fp32 sums; with bf16 tensors the softmax numerators are rounded to bf16 for the product with the values.  A row that sees no
- * key is zero.  What a row does not see takes no part in its result, whatever it holds (infinities and NaN included).  Outputs and workspace may overlap
+ * key is zero.  What a row does not see takes no part in its result, whatever it holds (infinities and NaN included); an infinity that it
+ * sees with a weight that fp32 holds as zero may make NaN.  Outputs and workspace may overlap
  * nothing else; calls that may run at the same time, on two streams or in two graphs, need a workspace each.
+ * How a call is launched is planned on the host, from its sequences, heads and rows and from table_pages * page_rows, the most rows that a sequence can have: with
+ * table_pages no larger than the call's longest sequence needs (table_stride as it is) a call over short sequences is often one launch where it would be two.
+ * Work is cut into even shares where there are few blocks of query rows x heads (at most 128 of 128 or 256, 1024 of 16 or 32, 512 with fp32 tensors); with more of
+ * them a sequence that is far longer than the others is better given a call of its own.
  */
 typedef struct sdllm_paged_shape {
   int32_t batch;        /* B >= 1 sequences */

@@ -8,9 +8,9 @@
 // of them are masked, is worked out in the matrix phase: causal with head_dim 64 240 us became 200.
 // Tiles that some row of a wave does not see all of are masked by 32 bits per row (seen_bits); whole tiles pay one scalar test.  Pages of the next 64 tiles are
 // looked up by one load, a tile per lane.
-// Rates, of 1245 TFLOP/s that a large product reaches: 4 x 4096 rows x 28/4 heads of 128, all keys seen, 1016 (without pages 1100), causal 970 to 990; four
-// prompts of 1024 to 4096 rows with a window of 1024 keys 720 (198 us; 7 of a workgroup's 45 us pass until its first logits, and the fifth round of workgroups is a
-// third full); head_dim 64, 8192 rows x 16/2 heads, causal, 855 (200 us, twice the exponentials per product).
+// Rates, of 1245 TFLOP/s that a large product reaches (two machines): 4 x 4096 rows x 28/4 heads of 128, all keys seen, 1070 (897 us; without pages 1100), causal
+// 925 to 995 (520 to 483); four prompts of 1024 to 4096 rows with a window of 1024 keys 695 to 720 (205 to 198; 7 of a workgroup's 45 us pass until its first logits,
+// and the fifth round of workgroups is a third full); head_dim 64, 8192 rows x 16/2 heads, causal, 815 to 855 (210 to 200, twice the exponentials per product).
 #include <type_traits>
 
 #include "attn_paged_merge.h"

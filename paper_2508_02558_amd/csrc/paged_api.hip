@@ -87,7 +87,9 @@ int32_t plan_paged(const sdllm_paged_shape_t& s, bool tree, PagedPlan& pl) {
   pl.least_tiles = few ? pl.waves : pl.shared ? 8 : f32 ? 2 * pl.waves : 6 * pl.waves;
   // With items for half the CUs, workgroups that share tiles are better left whole: a second round of them costs more than uneven items do (256 columns x 2000
   // keys: 128 items 57.5 us cut, 66.3 whole; 144 items 91.4, 67.0).  Streaming ones fit in between (320 items of 2000 keys 63.0 cut, 59.9 whole, of 1 to 8000
-  // keys 128, 151).
+  // keys 128, 151).  The rule counts items and does not know their lengths: with more of them, one sequence that is much longer than the others is not cut either
+  // (trees of 20 rows x 32/8 heads, 100000 rows among sequences of 500: 128 items 134 us, 136 items 1630; single tokens x 32/8 heads likewise: 1024 items 146,
+  // 1032 items 1237).
   pl.splits = items <= (pl.shared ? kNumCUs / 2 : 2 * at_once) && tiles > (few ? 4 * pl.waves - 1 : pl.least_tiles);
   pl.workgroups = pl.splits ? (int)std::max<int64_t>(at_once, 2 * items) : (int)whole;
   while (tiles >> pl.tile_shift >= 1 << 20) ++pl.tile_shift;   // items <= 1024
